@@ -34,6 +34,7 @@
  *                              per layer: hpd_rope_append  (or hpd_rope -> hpd_kv_append)
  *                                         -> hpd_attn_decode  (or _shared / _posorder)
  *                              hpd_advance  (once per step, after the last layer).
+ *     With paged caches in 8 bits hpd_append_paged -> hpd_attn_decode_paged take the layer's place.
  *     The first inference step over the prompt tokens is hpd_prefill_meta -> hpd_prefill_attn.
  */
 #ifndef HPD_H_
@@ -294,6 +295,61 @@ int hpd_prefill_attn(const hpd_geom* geom /*host*/, int n_docs, int total_tokens
                      const int32_t* doc_kv_start, const int32_t* doc_prefix_len, const int32_t* tok_doc, const int32_t* tok_vis,
                      const int32_t* n_tokens, void* o, float* lse,
                      void* workspace, size_t workspace_bytes, int32_t* dev_status, void* stream);
+
+/*
+ * Paged caches in 8 bits.  (The paper has no counterpart: its caches are dense and in the model's type.)  A cache is a pool of
+ * n_pages pages of page_size tokens.  A page holds, for every kv head, e4m3 codes of its keys and of its values and one scale each:
+ *   page_k, page_v              [n_pages, Hkv, page_size, D]  e4m3 (one byte: sign, 4 exponent bits, 3 fraction bits; no infinities)
+ *   page_k_scale, page_v_scale  [n_pages, Hkv]                e8m0 (one byte b: 2^(b-127); 255: NaN)
+ *   value = code * scale.  A cached element is within 2^-4 of itself of what was appended (2^-10 of the scale below 2^-6 of it).
+ * Sequences -- documents, branches -- own pages through a table int32 [table_rows, pages_per_seq]: token t of a sequence is token
+ * t % page_size of page table[t / page_size].  No two sequences that are appended to may own the same page; for reading, documents may share pages.
+ *
+ * hpd_append_paged -- new keys and values behind what their sequences hold, rotated on the way as by hpd_rope.
+ *   Two forms.  Tokens: row_seq[r] (dev) is the sequence of row r, seq_row_start[n_seqs+1] the first row of each sequence and the end
+ *   (rows of a sequence are consecutive); row r becomes token seq_len[s] + r - seq_row_start[s]; page_size <= 64.  This is the first step,
+ *   with doc tables of hpd_prefill_meta (tok_doc, doc_kv_start, tok_pos, n_tokens), and every further chunk.  Step: row_seq and
+ *   seq_row_start NULL: row r < n_rows is the one new token of sequence r, token seq_len[r].  This is the decode step, with
+ *   hpd_build_meta's tables (active_slot, suffix_len, pos_id, n_active).
+ *     n_rows [1] (dev)      rows in use (of max_rows; in the step form of n_seqs, too)
+ *     seq_id [n_seqs]       row of the page table of each sequence; NULL: its own number
+ *     seq_len [n_seqs]      tokens that the sequence held before the call; the caller advances it
+ *     pos_id [max_rows]     position IDs; NULL: keys are stored as they come (q and q_rot must be NULL then)
+ *     q, q_rot [max_rows, Hq, D] bf16: queries and where the rotated ones go (may be the same memory); both NULL: keys only
+ *     k_new, v_new [max_rows, Hkv, D] bf16, not changed
+ *   The rotated key is rounded to bf16 as by hpd_rope and quantised from there.  Scales are powers of two: for the tokens that a call puts
+ *   into a page, the smallest 2^n >= 2^-126 with (largest finite magnitude) <= 448 * 2^n; a page that held tokens keeps its scale where that is
+ *   larger, and where it is smaller the codes held are multiplied by the quotient and rounded.  Codes are rounded to nearest (even);
+ *   infinities become the largest code, NaN stays NaN.  Bytes of a page behind its last token are not touched.
+ *   A token beyond pages_per_seq * page_size sets HPD_S_OVERFLOW, a table entry out of range HPD_S_BAD_TABLE; nothing is stored for it, its q is rotated.
+ */
+int hpd_append_paged(const hpd_geom* geom /*host*/, int n_seqs, int max_rows, const int32_t* n_rows /*dev*/,
+                     const int32_t* row_seq, const int32_t* seq_row_start, const int32_t* seq_id, const int32_t* seq_len,
+                     const int32_t* page_table, int table_rows, int pages_per_seq, int n_pages, int page_size,
+                     const int32_t* pos_id, const void* q, void* q_rot, const void* k_new, const void* v_new,
+                     void* page_k, void* page_v, void* page_k_scale, void* page_v_scale, int32_t* dev_status, void* stream);
+
+/*
+ * hpd_attn_decode_paged -- hpd_attn_decode over paged caches in 8 bits: for row r (document d, slot s) and q head h
+ *     o = softmax(sm_scale * q . [K_d ; K_s]^T) [V_d ; V_s]
+ * over the document's doc_prefix_len[d] tokens in the pages that doc_page[d] names (page_size 16, 32 or 64) and the branch's tokens in
+ * page slot_page[s] of the branches' pool, whose pages hold suffix_cap tokens.  A document's pages are read from memory once per kv head for all
+ * of its rows.  Scores, softmax and sums are held in fp32; probabilities are rounded to fp16, codes enter the products exactly.
+ *   q [max_rows, Hq, D] bf16 (rotated); doc_page [n_docs, pages_per_doc], slot_page [n_slots] int32 (dev); tables and workspace from
+ *   hpd_build_meta (active_slot, suffix_len, ...); suffix_includes_new, o, lse as hpd_attn_decode.  Documents may share pages.
+ *   What lies in a page behind its last token, NaN included, has no influence.  A NaN code in a document's key or value reaches the rows of that document
+ *   alone, one of a branch that branch's rows alone (all of their elements); a row whose q holds an infinity or NaN is NaN.
+ *   A document's page out of range sets HPD_S_BAD_TABLE and makes that document's rows NaN; so does a document longer than
+ *   pages_per_doc * page_size.  A branch's page out of range sets HPD_S_BAD_TABLE and its rows see the document only.
+ */
+int hpd_attn_decode_paged(const hpd_geom* geom /*host*/, int n_docs, int max_rows, int n_slots, const void* q,
+                          const void* page_k, const void* page_v, const void* page_k_scale, const void* page_v_scale,
+                          const int32_t* doc_page, int pages_per_doc, int n_pages, int page_size,
+                          const void* branch_k, const void* branch_v, const void* branch_k_scale, const void* branch_v_scale,
+                          const int32_t* slot_page, int n_branch_pages,
+                          const int32_t* doc_prefix_len, const int32_t* doc_active_start, const int32_t* doc_id,
+                          const int32_t* active_slot, const int32_t* suffix_len, const int32_t* n_active, int suffix_includes_new,
+                          void* o, float* lse, void* workspace, size_t workspace_bytes, int32_t* dev_status, void* stream);
 
 /*
  * std_attn_decode -- the in-repo comparison: standard batched decode in which every branch is a

@@ -21,7 +21,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libhpd.so")
 
 EXPORTS = ("hpd_strerror", "hpd_last_cuda_error", "hpd_workspace_bytes", "hpd_build_meta", "hpd_rope",
-           "hpd_kv_append", "hpd_rope_append", "hpd_attn_decode", "hpd_build_meta_skeleton", "hpd_attn_decode_posorder", "hpd_advance", "hpd_merge_lse", "hpd_prefill_meta", "hpd_prefill_attn", "hpd_attn_decode_shared", "std_workspace_bytes", "std_attn_decode",
+           "hpd_kv_append", "hpd_rope_append", "hpd_attn_decode", "hpd_build_meta_skeleton", "hpd_attn_decode_posorder", "hpd_advance", "hpd_merge_lse", "hpd_prefill_meta", "hpd_prefill_attn", "hpd_attn_decode_shared", "hpd_append_paged", "hpd_attn_decode_paged", "std_workspace_bytes", "std_attn_decode",
            "std_attn_decode_static_max_bytes", "std_attn_decode_static")
 
 HPD_S_OVERFLOW, HPD_S_BAD_TABLE, HPD_S_TIMEOUT = 1, 2, 4
@@ -72,6 +72,11 @@ def load() -> C.CDLL:
         lib.hpd_attn_decode_shared.restype = C.c_int
         lib.hpd_attn_decode_shared.argtypes = [C.POINTER(HpdGeom), C.c_int, C.c_int, C.c_int, C.c_int] + [vp] * 7 + [C.c_int] + \
                                               [vp] * 10 + [C.c_int, vp, vp, vp, C.c_size_t, vp, vp]
+        lib.hpd_append_paged.restype = C.c_int
+        lib.hpd_append_paged.argtypes = [C.POINTER(HpdGeom), C.c_int, C.c_int] + [vp] * 6 + [C.c_int] * 4 + [vp] * 11
+        lib.hpd_attn_decode_paged.restype = C.c_int
+        lib.hpd_attn_decode_paged.argtypes = [C.POINTER(HpdGeom), C.c_int, C.c_int, C.c_int] + [vp] * 6 + [C.c_int] * 3 + [vp] * 5 + [C.c_int] + \
+                                             [vp] * 6 + [C.c_int, vp, vp, vp, C.c_size_t, vp, vp]
         lib.hpd_merge_lse.restype = C.c_int
         lib.hpd_merge_lse.argtypes = [C.POINTER(HpdGeom), C.c_int] + [vp] * 8
         lib.hpd_advance.restype = C.c_int
@@ -251,6 +256,76 @@ def hpd_attn_decode_shared(geom, n_docs, max_rows, n_slots, total_prefix_tokens,
                                          m.suffix_off, m.suffix_len, m.n_active, int(bool(suffix_includes_new)),
                                          o, lse, m.workspace, m.workspace.numel(), m.dev_status)
     _check(rc, "hpd_attn_decode_shared")
+
+
+@dataclass
+class PagedCache:
+    """A paged cache in 8 bits: pools of codes ``k``, ``v`` [n_pages, Hkv, page_size, D] (e4m3) with scales ``k_scale``, ``v_scale`` [n_pages,
+    Hkv] (e8m0: powers of two), and the ``table`` [sequences, pages_per_seq] (int32) that says which pages a sequence owns.  value = code * scale."""
+    k: torch.Tensor
+    v: torch.Tensor
+    k_scale: torch.Tensor
+    v_scale: torch.Tensor
+    table: torch.Tensor
+
+    def __post_init__(self):
+        if self.k.dim() != 4 or self.k.shape != self.v.shape or self.k.dtype != torch.float8_e4m3fn or self.v.dtype != torch.float8_e4m3fn:
+            raise HpdError("a paged cache's k and v are float8_e4m3fn [n_pages, Hkv, page_size, D], alike")
+        for x in (self.k_scale, self.v_scale):
+            if tuple(x.shape) != tuple(self.k.shape[:2]) or x.dtype != torch.float8_e8m0fnu:
+                raise HpdError("a paged cache's scales are float8_e8m0fnu [n_pages, Hkv]")
+        if self.table.dim() != 2 or self.table.dtype != torch.int32:
+            raise HpdError("a paged cache's table is int32 [sequences, pages_per_seq]")
+
+    @staticmethod
+    def alloc(geom, n_seqs: int, pages_per_seq: int, page_size: int, n_pages: Optional[int] = None, device="cuda") -> "PagedCache":
+        """An empty cache.  Without ``n_pages`` every sequence owns pages_per_seq pages of its own, in order; with it the pool is that large and the
+        table is left to the caller (-1: no page)."""
+        own = n_pages is None
+        n = n_seqs * pages_per_seq if own else n_pages
+        # (a pool keeps one page where it would be empty: an empty tensor has no address)
+        codes = [torch.zeros(max(n, 1), geom.Hkv, page_size, geom.D, dtype=torch.uint8, device=device).view(torch.float8_e4m3fn) for _ in range(2)]
+        scales = [torch.zeros(max(n, 1), geom.Hkv, dtype=torch.uint8, device=device).view(torch.float8_e8m0fnu) for _ in range(2)]
+        table = (torch.arange(n, dtype=torch.int32, device=device).view(n_seqs, pages_per_seq) if own else
+                 torch.full((n_seqs, pages_per_seq), -1, dtype=torch.int32, device=device))
+        return PagedCache(*codes, *scales, table)
+
+    @property
+    def n_pages(self) -> int:
+        return self.k.shape[0]
+
+    @property
+    def page_size(self) -> int:
+        return self.k.shape[2]
+
+    def check(self, geom, what: str):
+        if self.k.shape[1] != geom.Hkv or self.k.shape[3] != geom.D:
+            raise HpdError(f"{what}: the cache has {self.k.shape[1]} heads of {self.k.shape[3]} elements, the geometry {geom.Hkv} of {geom.D}")
+
+
+def hpd_append_paged(geom, n_seqs, max_rows, n_rows, row_seq, seq_row_start, seq_id, seq_len, cache: PagedCache, pos_id, q, q_rot, k_new, v_new,
+                     dev_status):
+    cache.check(geom, "hpd_append_paged")
+    rc = _calls().hpd_append_paged(geom, n_seqs, max_rows, n_rows, row_seq, seq_row_start, seq_id, seq_len, cache.table, cache.table.shape[0],
+                                   cache.table.shape[1], cache.k.shape[0], cache.k.shape[2], pos_id, q, q_rot, k_new, v_new, cache.k, cache.v,
+                                   cache.k_scale, cache.v_scale, dev_status)
+    _check(rc, "hpd_append_paged")
+
+
+def hpd_attn_decode_paged(geom, n_docs, max_rows, n_slots, q, docs: PagedCache, branches: PagedCache, doc_prefix_len, m: MetaTables,
+                          suffix_includes_new, o, lse=None):
+    docs.check(geom, "hpd_attn_decode_paged")
+    branches.check(geom, "hpd_attn_decode_paged")
+    if branches.page_size != geom.suffix_cap or tuple(branches.table.shape) != (n_slots, 1):
+        raise HpdError(f"hpd_attn_decode_paged: a branch owns one page of suffix_cap = {geom.suffix_cap} tokens (table [n_slots, 1]), got pages of "
+                       f"{branches.page_size} and a table {tuple(branches.table.shape)}")
+    if docs.table.shape[0] < n_docs:
+        raise HpdError(f"hpd_attn_decode_paged: the documents' table has {docs.table.shape[0]} rows for {n_docs} documents")
+    rc = _calls().hpd_attn_decode_paged(geom, n_docs, max_rows, n_slots, q, docs.k, docs.v, docs.k_scale, docs.v_scale, docs.table, docs.table.shape[1],
+                                        docs.k.shape[0], docs.k.shape[2], branches.k, branches.v, branches.k_scale, branches.v_scale, branches.table,
+                                        branches.k.shape[0], doc_prefix_len, m.doc_active_start, m.doc_id, m.active_slot, m.suffix_len, m.n_active,
+                                        int(bool(suffix_includes_new)), o, lse, m.workspace, m.workspace.numel(), m.dev_status)
+    _check(rc, "hpd_attn_decode_paged")
 
 
 def hpd_merge_lse(geom, max_rows, n_active, o_a, lse_a, o_b, lse_b, o, lse=None):

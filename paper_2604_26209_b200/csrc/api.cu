@@ -352,6 +352,74 @@ int hpd_prefill_attn(const hpd_geom* geom, int n_docs, int total_tokens,
                        workspace, workspace_bytes, dev_status, stream);
 }
 
+int hpd_append_paged(const hpd_geom* geom, int n_seqs, int max_rows, const int32_t* n_rows,
+                     const int32_t* row_seq, const int32_t* seq_row_start, const int32_t* seq_id, const int32_t* seq_len,
+                     const int32_t* page_table, int table_rows, int pages_per_seq, int n_pages, int page_size,
+                     const int32_t* pos_id, const void* q, void* q_rot, const void* k_new, const void* v_new,
+                     void* page_k, void* page_v, void* page_k_scale, void* page_v_scale, int32_t* dev_status, void* stream)
+{
+    int rc = geom_check(geom);
+    if (rc != HPD_OK) return rc;
+    if (n_seqs < 0 || max_rows < 0 || table_rows < 0 || pages_per_seq < 0 || n_pages < 0 || page_size < 1) return HPD_E_ARG;
+    if ((row_seq == nullptr) != (seq_row_start == nullptr) || (q == nullptr) != (q_rot == nullptr) || (q && !pos_id)) return HPD_E_ARG;
+    if (page_size > (row_seq ? 64 : kMaxPackedColumns)) return HPD_E_CAPACITY;
+    if (max_rows == 0 || n_seqs == 0) return HPD_OK;
+    if (!n_rows || !seq_len || !page_table || !k_new || !v_new || !page_k || !page_v || !page_k_scale || !page_v_scale) return HPD_E_ARG;
+    if (!aligned16(q) || !aligned16(q_rot) || !aligned16(k_new) || !aligned16(v_new) || !aligned16(page_k) || !aligned16(page_v)) return HPD_E_ARG;
+    const auto bf16 = [](const void* x) { return static_cast<const __nv_bfloat16*>(x); };
+    const auto bytes = [](void* x) { return static_cast<uint8_t*>(x); };
+    const AppendPagedArgs a{n_seqs, max_rows, table_rows, pages_per_seq, n_pages, page_size, n_rows, row_seq, seq_row_start, seq_id, seq_len,
+                            page_table, pos_id, bf16(q), static_cast<__nv_bfloat16*>(q_rot), bf16(k_new), bf16(v_new), bytes(page_k), bytes(page_v),
+                            bytes(page_k_scale), bytes(page_v_scale), dev_status, static_cast<cudaStream_t>(stream)};
+    return launch_append_paged(*geom, a);
+}
+
+int hpd_attn_decode_paged(const hpd_geom* geom, int n_docs, int max_rows, int n_slots, const void* q,
+                          const void* page_k, const void* page_v, const void* page_k_scale, const void* page_v_scale,
+                          const int32_t* doc_page, int pages_per_doc, int n_pages, int page_size,
+                          const void* branch_k, const void* branch_v, const void* branch_k_scale, const void* branch_v_scale,
+                          const int32_t* slot_page, int n_branch_pages,
+                          const int32_t* doc_prefix_len, const int32_t* doc_active_start, const int32_t* doc_id,
+                          const int32_t* active_slot, const int32_t* suffix_len, const int32_t* n_active, int suffix_includes_new,
+                          void* o, float* lse, void* workspace, size_t workspace_bytes, int32_t* dev_status, void* stream)
+{
+    int rc = geom_check(geom);
+    if (rc != HPD_OK) return rc;
+    if (!(geom->sm_scale > 0.f)) return HPD_E_GEOM;
+    if (n_docs < 0 || max_rows < 0 || n_slots < 0 || pages_per_doc < 0 || n_pages < 0 || n_branch_pages < 0) return HPD_E_ARG;
+    if (page_size != 16 && page_size != 32 && page_size != 64) return HPD_E_ARG;
+    if (attn_packed_columns(*geom) > kMaxPackedColumns) return HPD_E_CAPACITY;
+    // rows of codes (tokens x heads) are counted in 32 bits
+    const long long heads = geom->Hkv;
+    if (n_pages > 0x7fffffffll / (heads * page_size) || n_branch_pages > 0x7fffffffll / (heads * geom->suffix_cap)) return HPD_E_CAPACITY;
+    if (max_rows == 0 || n_docs == 0) return HPD_OK;
+    if (!q || !doc_prefix_len || !doc_active_start || !doc_id || !active_slot || !suffix_len || !n_active || !slot_page || !o || !workspace)
+        return HPD_E_ARG;
+    if (n_pages > 0 && (!page_k || !page_v || !page_k_scale || !page_v_scale)) return HPD_E_ARG;
+    if (pages_per_doc > 0 && !doc_page) return HPD_E_ARG;
+    if (n_branch_pages > 0 && (!branch_k || !branch_v || !branch_k_scale || !branch_v_scale)) return HPD_E_ARG;
+    if (!aligned16(q) || !aligned16(page_k) || !aligned16(page_v) || !aligned16(branch_k) || !aligned16(branch_v) || !aligned16(o) ||
+        !aligned16(workspace)) return HPD_E_ARG;
+    PagedArgs p{};
+    p.a.lay = ws_layout(*geom, n_docs, n_slots, sm_count());
+    if (workspace_bytes < p.a.lay.total) return HPD_E_WORKSPACE;
+    p.a.g = *geom;
+    p.a.n_docs = n_docs; p.a.max_rows = max_rows; p.a.n_slots = n_slots;
+    p.a.q = static_cast<const __nv_bfloat16*>(q);
+    p.a.doc_prefix_len = doc_prefix_len; p.a.doc_active_start = doc_active_start; p.a.doc_id = doc_id;
+    p.a.active_slot = active_slot; p.a.suffix_len = suffix_len; p.a.n_active = n_active;
+    p.a.suffix_extra = suffix_includes_new ? 1 : 0;
+    p.a.o = static_cast<__nv_bfloat16*>(o); p.a.lse = lse;
+    p.a.workspace = workspace; p.a.dev_status = dev_status; p.a.stream = static_cast<cudaStream_t>(stream);
+    const auto bytes = [](const void* x) { return static_cast<const uint8_t*>(x); };
+    p.page_k = bytes(page_k); p.page_v = bytes(page_v); p.scale_k = bytes(page_k_scale); p.scale_v = bytes(page_v_scale);
+    p.page_table = doc_page; p.pages_per_doc = pages_per_doc; p.n_pages = n_pages; p.page_size = page_size;
+    p.branch_k = bytes(branch_k); p.branch_v = bytes(branch_v);
+    p.branch_scale_k = bytes(branch_k_scale); p.branch_scale_v = bytes(branch_v_scale);
+    p.slot_page = slot_page; p.n_branch_pages = n_branch_pages;
+    return launch_attn_paged(p);
+}
+
 static int std_splits(const hpd_geom* g, int max_rows, int max_seq_len)
 {
     // one persistent CTA per SM takes (sequence, block of 8 kv heads, split) items: split long sequences when the

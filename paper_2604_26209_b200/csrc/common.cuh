@@ -111,6 +111,29 @@ struct AttnArgs {
     cudaStream_t stream;
 };
 
+// New tokens into pages of 8-bit codes (hpd_append_paged): row_seq and seq_row_start null: row r is sequence r's one token.
+struct AppendPagedArgs {
+    int n_seqs, max_rows, table_rows, pages_per_seq, n_pages, page_size;
+    const int32_t *n_rows, *row_seq, *seq_row_start, *seq_id, *seq_len, *page_table, *pos_id;
+    const __nv_bfloat16* q;          // null: keys only
+    __nv_bfloat16* q_rot;
+    const __nv_bfloat16 *k_new, *v_new;
+    uint8_t *page_k, *page_v, *scale_k, *scale_v;
+    int32_t* dev_status;
+    cudaStream_t stream;
+};
+
+// Attention over paged caches of 8-bit codes (hpd_attn_decode_paged).
+struct PagedArgs {
+    AttnArgs a;                      // geometry, row and document tables, outputs, workspace; its K/V pointers are null
+    const uint8_t *page_k, *page_v, *scale_k, *scale_v;              // documents: codes [n_pages, Hkv, page_size, D], scales [n_pages, Hkv]
+    const int32_t* page_table;       // [n_docs, pages_per_doc]
+    int pages_per_doc, n_pages, page_size;
+    const uint8_t *branch_k, *branch_v, *branch_scale_k, *branch_scale_v;    // branches: codes [n_branch_pages, Hkv, suffix_cap, D]
+    const int32_t* slot_page;        // [n_slots]
+    int n_branch_pages;
+};
+
 // Standard batched decode over private per-sequence K/V copies (std_attn_decode).
 struct StdArgs {
     hpd_geom g;
@@ -151,6 +174,8 @@ int launch_advance(const hpd_geom& g, int max_rows, const int32_t* n_active, con
                    int32_t* n_alive, cudaStream_t stream);
 int launch_merge_lse(const hpd_geom& g, int max_rows, const int32_t* n_active, const __nv_bfloat16* o_a, const float* lse_a,
                      const __nv_bfloat16* o_b, const float* lse_b, __nv_bfloat16* o, float* lse, cudaStream_t stream);
+int launch_append_paged(const hpd_geom& g, const AppendPagedArgs& a);
+int launch_attn_paged(const PagedArgs& p);
 int launch_attn_std(const StdArgs& a);         // TMA ring + warp-level tensor-core instructions
 int launch_attn_tc(const AttnArgs& a);       // tcgen05 / TMA kernel
 

@@ -98,7 +98,7 @@ PyObject* invoke(int (*f)(const hpd_geom*, A...), PyObject* const* args, Py_ssiz
 #define HPD_ENTRIES(X)                                                                                              \
     X(hpd_build_meta) X(hpd_build_meta_skeleton) X(hpd_rope) X(hpd_kv_append) X(hpd_rope_append) X(hpd_attn_decode)  \
     X(hpd_attn_decode_posorder) X(hpd_attn_decode_shared) X(hpd_advance) X(hpd_merge_lse) X(hpd_prefill_meta)        \
-    X(hpd_prefill_attn)
+    X(hpd_prefill_attn) X(hpd_append_paged) X(hpd_attn_decode_paged)
 
 #define X(name)                                                                                                     \
     decltype(&::name) at_##name = nullptr;                                                                          \

@@ -8,6 +8,7 @@
 #include <algorithm>
 
 #include "common.cuh"
+#include "rotary.cuh"
 
 namespace hpd {
 
@@ -25,11 +26,6 @@ template <bool FUSED> constexpr int kRopeResident = FUSED ? 6 : 8;   // CTAs of 
 // Every thread first asks for its share of the rows' q / k / v chunks (up to ten 16-byte loads in
 // flight per thread), then evaluates one of the rows' D/2 (cos, sin) pairs; they are kept in shared memory as fp32 and
 // applied to all Hq + Hkv heads: a thread rotates 8 pairs at a time from one 16-byte chunk of the low half and one of the high half.
-// Angles reach thousands of radians, where an fp32 product pos * inv_freq already loses ~1e-4 rad: the product and its
-// reduction to [-pi, pi] are taken in fp64 (inverse frequencies computed in fp64 on the host, 2*pi split in two doubles),
-// and only the reduced angle goes through the fp32 sine and cosine.
-struct InvFreq { double f[64]; };                    // theta^(-2i/D), i < D/2 <= 64
-
 struct AppendDst {                                   // fused kernel only: where the row's key and value go
     int32_t suffix_cap;
     int64_t cache_rows;
@@ -108,12 +104,8 @@ rope_kernel(int Hq, int Hkv, const InvFreq inv_freq, const int32_t* n_active,
 
     // ---- angles, and where each row goes in the branch cache (-1: slab full or table entry out of range -> status bit, no write) ----
     if (ar < nr) {
-        const double ang = static_cast<double>(pos) * inv_freq.f[ai];
-        const double k = rint(ang * 0.15915494309189535);                       // turns
-        double r = fma(-k, 6.283185307179586, ang);                             // minus k * 2*pi (high part, then the rest)
-        r = fma(-k, 2.4492935982947064e-16, r);
         float s, c;
-        sincosf(static_cast<float>(r), &s, &c);
+        rotary_angle(pos, inv_freq.f[ai], c, s);
         cs[ar][ai] = c;
         sn[ar][ai] = s;
     }
@@ -219,19 +211,6 @@ kv_append_kernel(int row_u4 /* Hkv*D*2/16 */, int32_t suffix_cap, int64_t cache_
         kd[i] = ks[i];
         vd[i] = vs[i];
     }
-}
-
-// Each thread keeps the table of its last (theta, D): a model asks for the same one layer after layer, and 64 powers take 3 us.
-const InvFreq& inv_freq_table(const hpd_geom& g)
-{
-    static thread_local InvFreq t;
-    static thread_local float theta = -1.f;
-    static thread_local int dim = 0;
-    if (g.rope_theta != theta || g.D != dim) {
-        for (int i = 0; i < g.D / 2; ++i) t.f[i] = pow(static_cast<double>(g.rope_theta), -2.0 * i / static_cast<double>(g.D));
-        theta = g.rope_theta; dim = g.D;
-    }
-    return t;
 }
 
 // End of a decode step (Sec. 4.3.4): PASSES rows per thread, whose loads (row -> slot -> depth) are all in flight before the first store.
