@@ -1,77 +1,950 @@
-// hpd_attn_decode_paged: one warp per (row, query head) over the document's pages and the branch's page, online softmax in fp32.
+// hpd_attn_decode_paged on the 5th-generation tensor cores: decode attention over paged caches of e4m3 codes.
+//
+// The structure is that of hpd_attn_decode: one persistent CTA per SM, two independent pipelines, each walking units of its own (up
+// to 128/G branches of a document x G query heads against a chunk of its prefix, for one kv head) in tiles of 64 keys, the
+// branches' own tokens first, packed back to back.  What differs is where the bytes are made into operands:
+//
+//   S = Q K^T    K tiles go from the pages to the tensor core as they are (kind::f8f6f4).  A row of q is scaled by a power of two, its
+//                largest magnitude to [128, 256), and split into two e4m3 terms, q = hi + lo: a bf16 has eight significant bits, two
+//                terms of four hold them all (below 2^-8 of the largest magnitude some are lost, at most 2^-17 of it).  Twice the
+//                k-steps at twice the rate of bf16, and no conversion of K.
+//   scales       a page's K scale multiplies its 16-column part of S inside the softmax's multiply-add, its V scale 2^e moves the
+//                exponent of its probabilities there: no instruction per element for either.
+//   O += P V     two warps of each pipeline widen V tiles from e4m3 to fp16 (exact) in shared memory; P is fp16 with its largest elements
+//                between 2^7 and 2^15, so that what is flushed is below 2^-31 of them.  They zero what lies behind a tile's last
+//                token, NaN codes included, and write the two terms of Q.
+//
+// Two references per row.  With s the scaled score (log2) and e the V exponent of its page, R >= s + e - 8 is what the products P V are
+// relative to (rescaled when it grows by more than 8), M >= s is what the sum is relative to.  A part of 16 columns whose products
+// stay below 2^-60 of R takes part in the sum alone: its probabilities are raised to there, where fp16 flushes them.
+//
+// Warps: 0 / 3 scheduler and copies of pipeline 0 / 1, 1 / 2 MMA issuers, 4-7 / 8-11 softmax, 12-13 / 14-15 conversion.
+// TMEM columns as in hpd_attn_decode: S0 [0,64) S1 [64,128) O [128,256) of a pipeline, P over the first half of its scores.
+// All waits are bounded: a wait that gives up raises HPD_S_TIMEOUT in the status word and the CTA drains and exits.
+#include <algorithm>
+#include <atomic>
+
+#include <cuda_fp16.h>
+
 #include "common.cuh"
 #include "paged.cuh"
+#include "ptx.cuh"
+#include "tc.cuh"
 
 namespace hpd {
 
 namespace {
 
+constexpr int kThreads = 512;
+constexpr int kM = 128;                    // rows of a tile
+constexpr int kN = 64;                     // keys of a tile
+constexpr int kPart = 16;                  // keys of a page at least: columns of S with one scale
+constexpr int kVHalf = kN * 128;           // one 64-element half of a widened V tile: 64 keys x 128 B
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+constexpr float kRescaleSlack = 8.0f;      // tolerated growth of the reference (log2 units) before O is rescaled
+constexpr float kUp = 7.0f;                // probabilities are 2^7 larger: 2^15 at most, fp16 holds 65504
+constexpr float kFaint = 60.0f;            // products below 2^-60 of the reference are dropped
+constexpr uint32_t kColPipe = 256, kColS = 0, kColO = 128;
+struct Regs { static constexpr int IO = 112, SOFTMAX = 168, CONVERT = 64; };
+static_assert(Regs::IO + 2 * Regs::SOFTMAX + Regs::CONVERT <= 4 * 128, "registers traded between the warpgroups exceed the CTA's allocation");
+constexpr int kRounds = 4;                 // a unit has at most 128 branches: 4 rounds of 32 lanes
+constexpr int kDescReaders = 7;            // MMA thread, four softmax warps, two conversion warps
+constexpr int kScaleSlots = 8;             // tiles whose scales are kept: more than the copies can run ahead of the softmax
+
+template <int D> struct Cfg {
+    static constexpr int Q_BYTES = kM * 2 * D;                   // two e4m3 terms of every element
+    static constexpr int KV_BYTES = kN * D;                      // one tile of codes
+    static constexpr int WIDE_BYTES = kN * 2 * D;                // one V tile in fp16
+    static constexpr int NK = D == 128 ? 3 : 4;                  // K stages of a pipeline
+    static constexpr int NC = D == 128 ? 3 : 4;                  // V stages as codes
+    static constexpr int NV = D == 128 ? 1 : 2;                  // V stages in fp16
+    static constexpr int PAD = D == 128 ? 1 : 2;                 // a branch begins at a multiple of PAD columns (a copy's destination: 128 bytes)
+    static constexpr int OFF_Q = 0;
+    static constexpr int OFF_STAGE = OFF_Q + 2 * Q_BYTES;        // output transpose, 2 KB per softmax warp
+    static constexpr int OFF_K = OFF_STAGE + 8 * 2048;
+    static constexpr int OFF_C = OFF_K + 2 * NK * KV_BYTES;
+    static constexpr int OFF_V = OFF_C + 2 * NC * KV_BYTES;
+    static constexpr int OFF_MISC = OFF_V + 2 * NV * WIDE_BYTES;
+    static constexpr int SMEM = OFF_MISC + 6144;
+    static_assert(OFF_V % 1024 == 0 && OFF_K % 1024 == 0, "swizzled tiles");
+    static_assert(NK + 2 < kScaleSlots, "scales are kept until the softmax has used them");
+};
+static_assert(Cfg<128>::SMEM <= 232448, "shared memory budget");
+
+struct Maps {
+    CUtensorMap page;                      // K codes of the documents: boxes of one page
+    CUtensorMap branch[16];                // K codes of the branches: boxes of 1 .. 16 tokens
+};
+
+struct Params {
+    PagedArgs a;
+    const WsHeader* hdr;
+    const WorkItem* work;
+    float *part_ml, *part_o;
+    float scale_log2;
+    int G;
+};
+
+struct UnitDesc {
+    int nt;                                // tiles of the unit (branches' and document's); -1: no more units
+    int np;                                // document's tiles
+    int stot;                              // packed columns of the branches
+    int head, key_count, part_base, row_begin, nb /*branches*/, row0 /*first global row*/;
+    int pad[7];
+    uint16_t cs[kM];                       // per branch: packed column of its first token
+    uint16_t len[kM];                      // per branch: tokens visible
+    uint8_t ks[kM], vs[kM];                // per branch: scale bytes of its page
+};
+static_assert(sizeof(UnitDesc) == 64 + 6 * kM, "descriptor size");
+
+constexpr int kMaxStages = 4;
+struct Misc {
+    unsigned long long q_full[2], q_empty[2];
+    unsigned long long k_full[2][kMaxStages], k_empty[2][kMaxStages], c_full[2][kMaxStages], c_empty[2][kMaxStages], v_full[2][kMaxStages], v_empty[2][kMaxStages];
+    unsigned long long s_full[2][2], p_full[2][2], p_empty[2][2], o_full[2], o_free[2];
+    unsigned long long desc_full[2], desc_empty[2], scale_full[2][kScaleSlots];
+    uint32_t tmem_base;
+    int abort_flag;
+    int pad[2];
+    float4 scale_k[2][kScaleSlots], exp_v[2][kScaleSlots];       // of a document's tile: K scale and V exponent of every 16 columns
+    float q_factor[2][kM];                 // what the scaled rows of q have to be multiplied by
+    uint32_t nan_branch[2][2][2][4];       // pipeline, unit's parity, conversion warp: branches with a NaN among their values
+    UnitDesc desc[2];
+};
+static_assert(sizeof(Misc) <= 6144, "misc block");
+
+// tcgen05.mma on two operands of e4m3 codes in shared memory (descriptors' low and high words)
+__device__ __forceinline__ void tc_mma_codes(uint32_t d_tmem, uint32_t a_lo, uint32_t a_hi, uint32_t b_lo, uint32_t b_hi, uint32_t idesc, uint32_t accumulate) {
+    asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\t"
+                 "mov.b64 da, {%1, %5};\n\tmov.b64 db, {%2, %6};\n\tsetp.ne.b32 p, %4, 0;\n\t"
+                 "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], da, db, %3, p;\n\t}"
+                 ::"r"(d_tmem), "r"(a_lo), "r"(b_lo), "r"(idesc), "r"(accumulate), "r"(a_hi), "r"(b_hi) : "memory");
+}
+// Descriptors' high words: SBO (bytes of eight rows / 16), version 1, swizzle mode: rows of 128 bytes (mode 2) or of 64 bytes (mode 4).
+constexpr uint32_t kRows128 = 0x40004040u, kRows64 = 0x80004020u;
+__device__ __forceinline__ uint32_t desc_lo(uint32_t saddr) { return (saddr >> 4) | (1u << 16); }
+__device__ __forceinline__ uint32_t desc_lo_mnmajor(uint32_t saddr) { return (saddr >> 4) | (static_cast<uint32_t>(kVHalf >> 4) << 16); }
+// Instruction descriptors, fp32 accumulation, M = 128: e4m3 x e4m3 with both K-major, fp16 x fp16 with B MN-major.
+__device__ __forceinline__ uint32_t idesc_codes(int N) { return (1u << 4) | (static_cast<uint32_t>(N >> 3) << 17) | (static_cast<uint32_t>(kM >> 4) << 24); }
+__device__ __forceinline__ uint32_t idesc_wide(int N) { return idesc_codes(N) | (1u << 16); }
+
+struct Unit { int nt, np, stot, head, key_count, part_base, row_begin, nb, row0; };
+__device__ __forceinline__ Unit read_unit(const UnitDesc& d) {
+    return {d.nt, d.np, d.stot, d.head, d.key_count, d.part_base, d.row_begin, d.nb, d.row0};
+}
+
 template <int D>
-__global__ void __launch_bounds__(256)
-attn_paged_kernel(const PagedArgs p, float scale)
+__global__ void __launch_bounds__(kThreads, 1)
+attn_paged_kernel(const __grid_constant__ Maps maps, const Params p)
 {
-    constexpr int E = D / 32;
-    const int Hq = p.a.g.Hq, Hkv = p.a.g.Hkv, G = Hq / Hkv, lane = threadIdx.x & 31;
-    const int64_t w = static_cast<int64_t>(blockIdx.x) * 8 + (threadIdx.x >> 5);
-    if (w >= static_cast<int64_t>(min(*p.a.n_active, p.a.max_rows)) * Hq) return;
-    const int r = static_cast<int>(w / Hq), h = static_cast<int>(w % Hq), kh = h / G;
-    float q[E], acc[E], m = -INFINITY, l = 0.f;
-    bool bad = false;
-    for (int e = 0; e < E; ++e) {
-        q[e] = __bfloat162float(p.a.q[w * D + lane * E + e]);
-        acc[e] = 0.f;
-        bad |= !(fabsf(q[e]) < INFINITY);
+    using C = Cfg<D>;
+    extern __shared__ __align__(1024) uint8_t smem[];
+    Misc* misc = reinterpret_cast<Misc*>(smem + C::OFF_MISC);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int G = p.G, Hkv = p.a.a.g.Hkv;
+    int32_t* status = p.a.a.dev_status;
+    if ((smem_u32(smem) & 1023u) != 0) {                 // swizzled tiles need 1024-byte alignment: refuse rather than misread
+        if (threadIdx.x == 0 && status) atomicOr(status, HPD_S_BAD_TABLE);
+        return;
     }
-    bad = __any_sync(0xffffffffu, bad);
-    auto token = [&](const uint8_t* k, const uint8_t* v, float ks, float vs) {
-        float s = 0.f;
-        for (int e = 0; e < E; ++e) s = fmaf(q[e], e4m3x2_value(k[lane * E + e]).x, s);
-        for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-        s *= ks * scale;
-        const float mn = fmaxf(m, s), f = m == -INFINITY ? 0.f : exp2f((m - mn)), pr = exp2f(s - mn);
-        l = l * f + pr;
-        for (int e = 0; e < E; ++e) acc[e] = acc[e] * f + pr * e4m3x2_value(v[lane * E + e]).x * vs;
-        m = mn;
-    };
-    const int d = p.a.doc_id[r];
-    int status = 0;
-    for (int t = 0; t < p.a.doc_prefix_len[d]; ++t) {
-        const int i = t / p.page_size;
-        const int page = i < p.pages_per_doc ? p.page_table[static_cast<int64_t>(d) * p.pages_per_doc + i] : -1;
-        if (page < 0 || page >= p.n_pages) { status = HPD_S_BAD_TABLE; bad = true; break; }
-        const int64_t ph = static_cast<int64_t>(page) * Hkv + kh, at = (ph * p.page_size + t % p.page_size) * D;
-        token(p.page_k + at, p.page_v + at, e8m0_value(p.scale_k[ph]), e8m0_value(p.scale_v[ph]));
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&misc->q_full[i], 2);  mbar_init(&misc->q_empty[i], 5);
+            for (int b = 0; b < 2; ++b) { mbar_init(&misc->s_full[i][b], 1); mbar_init(&misc->p_full[i][b], 4); mbar_init(&misc->p_empty[i][b], 1); }
+            mbar_init(&misc->o_full[i], 1);  mbar_init(&misc->o_free[i], 4);
+            mbar_init(&misc->desc_full[i], 1); mbar_init(&misc->desc_empty[i], kDescReaders);
+            for (int k = 0; k < kMaxStages; ++k) {
+                mbar_init(&misc->k_full[i][k], 1); mbar_init(&misc->k_empty[i][k], 1);
+                mbar_init(&misc->c_full[i][k], 1); mbar_init(&misc->c_empty[i][k], 2);
+                mbar_init(&misc->v_full[i][k], 2); mbar_init(&misc->v_empty[i][k], 1);
+            }
+            for (int k = 0; k < kScaleSlots; ++k) mbar_init(&misc->scale_full[i][k], 1);
+        }
+        misc->abort_flag = 0;
+        fence_mbar_init();
     }
-    const int n = max(0, min(p.a.suffix_len[r] + p.a.suffix_extra, p.a.g.suffix_cap));
-    const int slot = p.a.active_slot[r];
-    const int page = slot >= 0 && slot < p.a.n_slots ? p.slot_page[slot] : -1;
-    if (n > 0 && (page < 0 || page >= p.n_branch_pages)) {
-        status = HPD_S_BAD_TABLE;
+    // stale contents of widened tiles are multiplied by zero probabilities: they must be finite from the start
+    for (int i = threadIdx.x; i < (C::OFF_MISC - C::OFF_V) / 16; i += kThreads)
+        reinterpret_cast<uint4*>(smem + C::OFF_V)[i] = make_uint4(0, 0, 0, 0);
+    fence_async_smem();
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&misc->tmem_base)), "r"(512) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(&misc->tmem_base);
+
+    if (warp == 0 || warp == 3) {
+        // ============================ scheduler and copies of one pipeline =====================
+        // Units are drawn as in hpd_attn_decode: six fixed ones per pipeline, then from the step's ticket counter.  What a unit needs to
+        // know is a chain of loads -- item, row tables, pages, scales -- of which the unit before issues one link at a time between
+        // its tiles.
+        reg_dealloc<Regs::IO>();
+        const int x = warp == 0 ? 0 : 1;
+        const int n_units = p.hdr->n_work * Hkv;
+        const int P = p.a.page_size, shift = 31 - __clz(P);          // tokens of a page: 2^shift
+        const int per_tile = kN >> shift;                            // pages of a tile
+        const int per_batch = 32 / per_tile;                         // tiles whose pages the lanes hold
+        uint32_t* ticket = const_cast<uint32_t*>(&p.hdr->ticket);
+        UnitDesc& d = misc->desc[x];
+        uint8_t* k_ring = smem + C::OFF_K + x * C::NK * C::KV_BYTES;
+        uint8_t* c_ring = smem + C::OFF_C + x * C::NC * C::KV_BYTES;
+        if (n_units == 0) {
+            if (lane == 0) { d.nt = -1; mbar_arrive(&misc->desc_full[x]); }
+        } else {
+        constexpr int kStatic = 6;
+        const bool alternate = p.hdr->longest_first != 0;
+        const bool spread = n_units < 4 * 2 * static_cast<int>(gridDim.x);
+        const uint32_t first_dynamic = static_cast<uint32_t>(kStatic) * 2u * gridDim.x;
+        auto next = [&](int i) {                                     // the pipeline's i-th unit
+            uint32_t t = 0;
+            if (i < kStatic) {
+                const uint32_t j = spread ? blockIdx.x + static_cast<uint32_t>(x) * gridDim.x : 2u * blockIdx.x + static_cast<uint32_t>(x);
+                t = (((i & 1) && alternate) ? 2u * gridDim.x - 1u - j : j) + static_cast<uint32_t>(i) * 2u * gridDim.x;
+            } else {
+                if (lane == 0) t = atomicAdd(ticket, 1u);
+                t = __shfl_sync(0xffffffffu, t, 0) + first_dynamic;
+            }
+            return static_cast<int>(min(t, static_cast<uint32_t>(n_units)));
+        };
+        auto item_of = [&](int w) { return p.work[min(w, n_units - 1) / Hkv]; };
+        // ---- the links of a unit's chain: row tables and page numbers; branches' pages; scales ----
+        int len[kRounds], page[kRounds], ks[kRounds], vs[kRounds];   // per branch; page: slot, then page, then first row of its codes
+        int doc_row, bad;                                            // first row of the document; a table entry out of range
+        // per lane: one of 32 pages of the document: its number (-2: not needed), then first row of its codes (-1: none) and scale bytes
+        int id, row, sk, sv;
+        auto page_id = [&](const WorkItem& it, int i) {
+            const int at = (it.key_begin >> shift) + i;
+            if (i << shift >= it.key_count) return -2;
+            return at < p.a.pages_per_doc ? p.a.page_table[static_cast<int64_t>(it.doc) * p.a.pages_per_doc + at] : -1;
+        };
+        auto page_scales = [&](int id_, int head, int& row_, int& sk_, int& sv_) {
+            row_ = -1; sk_ = 127; sv_ = 127;
+            if (id_ == -2) return;
+            if (id_ < 0 || id_ >= p.a.n_pages) { sk_ = 255; bad = 1; return; }      // NaN for the document's rows
+            const int64_t ph = static_cast<int64_t>(id_) * Hkv + head;
+            row_ = static_cast<int>(ph << shift);
+            sk_ = p.a.scale_k[ph]; sv_ = p.a.scale_v[ph];
+        };
+        auto link_rows = [&](int w, const WorkItem& it, int das) {
+#pragma unroll
+            for (int r = 0; r < kRounds; ++r) {
+                const int b = lane + 32 * r;
+                len[r] = 0; page[r] = -1;
+                if (w < n_units && it.with_suffix && b < it.row_count) {
+                    len[r] = p.a.a.suffix_len[das + it.row_begin + b];
+                    page[r] = p.a.a.active_slot[das + it.row_begin + b];
+                }
+            }
+            id = w < n_units ? page_id(it, lane) : -2;
+        };
+        auto link_pages = [&]() {
+            bad = 0;
+#pragma unroll
+            for (int r = 0; r < kRounds; ++r) {
+                const int n = len[r] + p.a.a.suffix_extra;
+                len[r] = n < 0 ? 0 : n > p.a.a.g.suffix_cap ? p.a.a.g.suffix_cap : n;
+                if (page[r] < 0) len[r] = 0;
+                if (len[r] > 0) page[r] = page[r] < p.a.a.n_slots ? p.a.slot_page[page[r]] : -1;
+            }
+        };
+        auto link_scales = [&](int w) {
+            const int head = w % Hkv;
+#pragma unroll
+            for (int r = 0; r < kRounds; ++r) {
+                ks[r] = vs[r] = 127;
+                if (len[r] > 0) {
+                    if (page[r] < 0 || page[r] >= p.a.n_branch_pages) {
+                        bad = 1; len[r] = 0;
+                    } else {
+                        const int64_t ph = static_cast<int64_t>(page[r]) * Hkv + head;
+                        ks[r] = p.a.branch_scale_k[ph]; vs[r] = p.a.branch_scale_v[ph];
+                        page[r] = static_cast<int>(ph * p.a.a.g.suffix_cap);
+                    }
+                }
+            }
+            page_scales(id, head, row, sk, sv);
+        };
+        int w0 = next(0), w1 = next(1);
+        WorkItem it0 = item_of(w0), it1 = item_of(w1);
+        doc_row = it0.doc_row;
+        link_rows(w0, it0, doc_row);
+        link_pages();
+        link_scales(w0);
+        uint32_t kc = 0;                                             // tiles so far
+        bool ok = true;
+        for (uint32_t ui = 0; ok; ++ui) {
+            // ---- scan and publish unit ui ----
+            if (ui >= 1) {
+                ok = mbar_wait_warp(&misc->desc_empty[x], (ui - 1) & 1, misc);
+                if (!ok) break;
+            }
+            const bool live = w0 < n_units;
+            if (__any_sync(0xffffffffu, bad) && lane == 0 && status) atomicOr(status, HPD_S_BAD_TABLE);
+            int cs[kRounds];
+            int carry = 0;
+#pragma unroll
+            for (int r = 0; r < kRounds; ++r) {
+                const int b = lane + 32 * r;
+                const int occ = (len[r] + C::PAD - 1) / C::PAD * C::PAD;
+                int incl = occ;
+#pragma unroll
+                for (int s = 1; s < 32; s <<= 1) {
+                    const int v = __shfl_up_sync(0xffffffffu, incl, s);
+                    if (lane >= s) incl += v;
+                }
+                cs[r] = carry + incl - occ;
+                d.cs[b] = static_cast<uint16_t>(cs[r]);
+                d.len[b] = static_cast<uint16_t>(len[r]);
+                d.ks[b] = static_cast<uint8_t>(ks[r]);
+                d.vs[b] = static_cast<uint8_t>(vs[r]);
+                carry += __shfl_sync(0xffffffffu, incl, 31);
+            }
+            const int nrounds = ((live && it0.with_suffix ? it0.row_count : 0) + 31) >> 5;
+            const int ns = (carry + kN - 1) / kN, np = live ? (it0.key_count + kN - 1) / kN : 0;
+            const int nt = live ? ns + np : -1, head = w0 % Hkv;
+            if (lane == 0) {
+                d.nt = nt; d.np = np; d.stot = carry; d.head = head; d.key_count = it0.key_count; d.part_base = it0.part_base;
+                d.row_begin = it0.row_begin; d.nb = it0.row_count; d.row0 = doc_row + it0.row_begin;
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&misc->desc_full[x]);
+            if (!live) break;
+            // this unit's chain moves out of the way of the next one's
+            int blen[kRounds], brow[kRounds];
+#pragma unroll
+            for (int r = 0; r < kRounds; ++r) { blen[r] = len[r]; brow[r] = page[r]; }
+            int cur_row = row, cur_sk = sk, cur_sv = sv;             // this unit's batch of 32 pages, and the next
+            int nxt_id = page_id(it0, 32 + lane), nxt_row = -1, nxt_sk = 127, nxt_sv = 127;
+            const int w2 = next(static_cast<int>(ui) + 2);
+            const WorkItem it2 = item_of(w2);
+            doc_row = it1.doc_row;
+            link_rows(w1, it1, doc_row);
+            for (int t = 0; t < nt && ok; ++t, ++kc) {
+                const uint32_t st = kc % C::NK, sc = kc % C::NC, slot = kc % kScaleSlots;
+                uint8_t* kt = k_ring + st * C::KV_BYTES;
+                uint8_t* ct = c_ring + sc * C::KV_BYTES;
+                unsigned long long *kf = &misc->k_full[x][st], *cf = &misc->c_full[x][sc];
+                if (t < ns) {
+                    // pieces of the branches that fall into the tile; a box has the exact height of the piece
+                    const int c_lo = t * kN, c_hi = min(carry, c_lo + kN);
+                    int mine = 0;
+#pragma unroll
+                    for (int r = 0; r < kRounds; ++r) mine += max(0, min(cs[r] + blen[r], c_hi) - max(cs[r], c_lo));
+                    const uint32_t bytes = __reduce_add_sync(0xffffffffu, mine) * D;
+                    ok = mbar_wait_warp(&misc->k_empty[x][st], ((kc / C::NK) & 1) ^ 1, misc);
+                    if (!ok) break;
+                    if (lane == 0) mbar_expect_tx(kf, bytes);
+#pragma unroll
+                    for (int r = 0; r < kRounds; ++r) {
+                        if (r >= nrounds) break;
+                        const int lo = max(cs[r], c_lo);
+                        int n = min(cs[r] + blen[r], c_hi) - lo, from = brow[r] + (lo - cs[r]), col = lo - c_lo;
+                        while (n > 0) {
+                            const int hb = min(n, 16);
+                            tma_load_2d(kt + col * D, &maps.branch[hb - 1], kf, 0, from);
+                            from += hb; col += hb; n -= hb;
+                        }
+                    }
+                    if (lane == 0) mbar_arrive(&misc->scale_full[x][slot]);
+                    __syncwarp();
+                    ok = mbar_wait_warp(&misc->c_empty[x][sc], ((kc / C::NC) & 1) ^ 1, misc);
+                    if (!ok) break;
+                    if (lane == 0) mbar_expect_tx(cf, bytes);
+#pragma unroll
+                    for (int r = 0; r < kRounds; ++r) {
+                        if (r >= nrounds) break;
+                        const int lo = max(cs[r], c_lo), n = min(cs[r] + blen[r], c_hi) - lo;
+                        if (n > 0) bulk_load(ct + (lo - c_lo) * D, p.a.branch_v + static_cast<int64_t>(brow[r] + (lo - cs[r])) * D, cf, static_cast<uint32_t>(n) * D);
+                    }
+                } else {
+                    const int tp = t - ns, in_batch = tp % per_batch;
+                    if (tp > 0 && in_batch == 0) {                   // the next 32 pages; ask for the ones behind them
+                        cur_row = nxt_row; cur_sk = nxt_sk; cur_sv = nxt_sv;
+                        nxt_id = page_id(it0, (tp / per_batch + 1) * 32 + lane);
+                    }
+                    const int pages = (min(kN, it0.key_count - tp * kN) + P - 1) >> shift;
+                    const int l0 = in_batch * per_tile;              // lane of the tile's first page
+                    // scales of the tile's four parts
+                    const int from = l0 + ((lane & 3) * kPart >> shift);
+                    const int pk = __shfl_sync(0xffffffffu, cur_sk, from), pv = __shfl_sync(0xffffffffu, cur_sv, from);
+                    const unsigned have = __ballot_sync(0xffffffffu, cur_row >= 0) >> l0 & ((1u << pages) - 1u);
+                    const uint32_t bytes = static_cast<uint32_t>(__popc(have)) * P * D;
+                    ok = mbar_wait_warp(&misc->k_empty[x][st], ((kc / C::NK) & 1) ^ 1, misc);
+                    if (!ok) break;
+                    if (lane < 4) {
+                        reinterpret_cast<float*>(&misc->scale_k[x][slot])[lane] = e8m0_value(pk);
+                        reinterpret_cast<float*>(&misc->exp_v[x][slot])[lane] = pv == 255 ? __uint_as_float(0x7fffffffu) : static_cast<float>(pv - 127);
+                    }
+                    if (lane == 0) mbar_expect_tx(kf, bytes);
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&misc->scale_full[x][slot]);
+                    // the lanes that hold the tile's pages copy them
+                    const int j = lane - l0;
+                    const bool copies = j >= 0 && j < pages && cur_row >= 0;
+                    if (copies) tma_load_2d(kt + j * P * D, &maps.page, kf, 0, cur_row);
+                    __syncwarp();
+                    ok = mbar_wait_warp(&misc->c_empty[x][sc], ((kc / C::NC) & 1) ^ 1, misc);
+                    if (!ok) break;
+                    if (lane == 0) mbar_expect_tx(cf, bytes);
+                    if (copies) bulk_load(ct + j * P * D, p.a.page_v + static_cast<int64_t>(cur_row) * D, cf, static_cast<uint32_t>(P) * D);
+                    if (in_batch == 1) {
+                        const int was = bad;
+                        bad = 0;
+                        page_scales(nxt_id, head, nxt_row, nxt_sk, nxt_sv);
+                        if (__any_sync(0xffffffffu, bad) && lane == 0 && status) atomicOr(status, HPD_S_BAD_TABLE);
+                        bad = was;
+                    }
+                }
+                __syncwarp();
+                if (t == 0) link_pages();
+            }
+            if (!ok) break;
+            if (nt == 0) link_pages();
+            link_scales(w1);
+            w0 = w1; w1 = w2; it0 = it1; it1 = it2;
+        }
+        }
+    } else if (warp < 3) {
+        // ================================ MMA issuers (one per pipeline) =============================
+        reg_dealloc<Regs::IO>();
+        if (elect_one()) {
+            const int x = warp - 1;
+            uint32_t qc = 0, tiles = 0;                   // units with tiles so far; tiles of earlier units
+            uint32_t sc = 0, pc = 0;                      // S tiles issued, P tiles consumed
+            bool ok = true;
+            constexpr uint32_t kHi = D == 128 ? kRows128 : kRows64;
+            const uint32_t q_lo = desc_lo(smem_u32(smem + C::OFF_Q + x * C::Q_BYTES));
+            const uint32_t k_lo0 = desc_lo(smem_u32(smem + C::OFF_K + x * C::NK * C::KV_BYTES));
+            const uint32_t v_lo0 = desc_lo_mnmajor(smem_u32(smem + C::OFF_V + x * C::NV * C::WIDE_BYTES));
+            const uint32_t tmem_s = tmem + x * kColPipe + kColS, tmem_o = tmem + x * kColPipe + kColO;
+            const uint32_t idesc_pv = idesc_wide(D);
+            for (uint32_t ui = 0; ok; ++ui) {
+                ok = mbar_wait(&misc->desc_full[x], ui & 1, misc);
+                if (!ok) break;
+                const Unit u = read_unit(misc->desc[x]);
+                mbar_arrive(&misc->desc_empty[x]);
+                if (u.nt < 0) break;
+                const int nt = u.nt;
+                if (nt == 0) continue;
+                const int ns = nt - u.np;
+                const int last_s = u.stot - (ns - 1) * kN, last_p = u.key_count - (u.np - 1) * kN;
+                auto cols16 = [&](int j) {                // sixteens of columns of tile j
+                    int c = kN;
+                    if (j == ns - 1) c = last_s;
+                    else if (j == nt - 1) c = last_p;
+                    return (c + 15) >> 4;
+                };
+                ok = mbar_wait(&misc->q_full[x], qc & 1, misc);
+                ++qc;
+                auto issue_qk = [&](int j) {
+                    const uint32_t kt = tiles + j;
+                    const int ks = kt % C::NK;
+                    const uint32_t idesc = idesc_codes(cols16(j) << 4);
+                    const uint32_t k_lo = k_lo0 + ks * (C::KV_BYTES >> 4);
+                    if (!mbar_wait(&misc->k_full[x][ks], (kt / C::NK) & 1, misc)) return false;
+                    tc_fence_after();
+                    // k-steps of 32 codes; the low terms of q are a tile (D = 128) or half a row (D = 64) behind the high ones
+#pragma unroll
+                    for (int k = 0; k < 2 * D / 32; ++k) {
+                        const uint32_t kk = (k % (D / 32)) * 2;
+                        const uint32_t qk = k < D / 32 ? kk : (D == 128 ? (kM * 128 >> 4) + kk : 4 + kk);
+                        tc_mma_codes(tmem_s + (sc & 1) * kN, q_lo + qk, kRows128, k_lo + kk, kHi, idesc, k > 0);
+                    }
+                    tc_commit(&misc->k_empty[x][ks]);
+                    tc_commit(&misc->s_full[x][sc & 1]);
+                    if (j + 1 >= nt) tc_commit(&misc->q_empty[x]);
+                    ++sc;
+                    return true;
+                };
+                if (ok) ok = issue_qk(0);
+                if (ok && nt > 1) ok = issue_qk(1);
+                for (int j = 0; j < nt && ok; ++j) {
+                    const uint32_t vt = tiles + j;
+                    const int vs = vt % C::NV;
+                    const uint32_t v_lo = v_lo0 + vs * (C::WIDE_BYTES >> 4);
+                    const int nk = cols16(j);
+                    const uint32_t acc0 = j >= 1;
+                    const int pb = pc & 1;
+                    ok = mbar_wait(&misc->p_full[x][pb], (pc >> 1) & 1, misc);
+                    if (!ok) break;
+                    ok = mbar_wait(&misc->v_full[x][vs], (vt / C::NV) & 1, misc);
+                    if (!ok) break;
+                    if (j == 0 && qc > 1) {               // the epilogue of the unit before has read O
+                        ok = mbar_wait(&misc->o_free[x], (qc - 2) & 1, misc);
+                        if (!ok) break;
+                    }
+                    tc_fence_after();
+#pragma unroll
+                    for (int k = 0; k < kN / 16; ++k)
+                        if (k < nk) tc_mma_ts(tmem_o, tmem_s + pb * kN + k * 8, v_lo + k * 128, idesc_pv, k > 0 ? 1u : acc0);
+                    tc_commit(&misc->v_empty[x][vs]);
+                    tc_commit(&misc->p_empty[x][pb]);
+                    if (j + 1 >= nt) tc_commit(&misc->o_full[x]);
+                    ++pc;
+                    if (j + 2 < nt) ok = issue_qk(j + 2);
+                }
+                tiles += nt;
+            }
+        }
+    } else if (warp >= 12) {
+        // ======================= conversion: the two terms of Q, V tiles from e4m3 to fp16 ===================
+        reg_dealloc<Regs::CONVERT>();
+        const int x = (warp - 12) >> 1, half = warp & 1, tid = half * 32 + lane;
+        uint8_t* q_tile = smem + C::OFF_Q + x * C::Q_BYTES;
+        const uint8_t* c_ring = smem + C::OFF_C + x * C::NC * C::KV_BYTES;
+        uint8_t* v_ring = smem + C::OFF_V + x * C::NV * C::WIDE_BYTES;
+        uint32_t tiles = 0, qc = 0;
+        bool ok = true;
+        for (uint32_t ui = 0; ok; ++ui) {
+            ok = mbar_wait_warp(&misc->desc_full[x], ui & 1, misc);
+            if (!ok) break;
+            const UnitDesc& d = misc->desc[x];
+            const Unit u = read_unit(d);
+            uint32_t cols[kRounds];                       // of this lane's branches: first column and length, for NaN codes
+#pragma unroll
+            for (int r = 0; r < kRounds; ++r) cols[r] = d.cs[lane + 32 * r] | static_cast<uint32_t>(d.len[lane + 32 * r]) << 16;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&misc->desc_empty[x]);
+            if (u.nt < 0) break;
+            if (u.nt == 0) continue;
+            // ---- Q: a row by D/8 lanes, 16 bytes each; a batch of rows is in flight before the tile is free ----
+            constexpr int LANES = D / 8, ROWS = 32 / LANES, BATCH = 6;
+            const int nrows = u.nb * G, part = lane % LANES;
+            uint4 buf[BATCH];
+            auto row_of = [&](int i) { return (2 * i + half) * ROWS + lane / LANES; };
+            auto fetch = [&](int i0) {
+#pragma unroll
+                for (int i = 0; i < BATCH; ++i) {
+                    const int r = row_of(i0 + i), b = r / G, row = u.row0 + b;
+                    buf[i] = make_uint4(0, 0, 0, 0);
+                    if (r < nrows && row < p.a.a.max_rows)
+                        buf[i] = *reinterpret_cast<const uint4*>(p.a.a.q + (static_cast<int64_t>(row) * p.a.a.g.Hq + u.head * G + (r - b * G)) * D + part * 8);
+                }
+            };
+            fetch(0);
+            ok = mbar_wait_warp(&misc->q_empty[x], (qc & 1) ^ 1, misc);
+            if (!ok) break;
+            if (lane < 4) misc->nan_branch[x][qc & 1][half][lane] = 0u;
+            for (int i0 = 0; row_of(i0) - lane / LANES < nrows; i0 += BATCH) {
+                if (i0 > 0) fetch(i0);
+#pragma unroll
+                for (int i = 0; i < BATCH; ++i) {
+                    const int r = row_of(i0 + i);
+                    const uint32_t* w = reinterpret_cast<const uint32_t*>(&buf[i]);
+                    int top = 0;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) top = max(top, max(static_cast<int>(w[k] & 0x7fff), static_cast<int>(w[k] >> 16 & 0x7fff)));
+#pragma unroll
+                    for (int s = 1; s < LANES; s <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, s));
+                    if (r >= nrows) continue;
+                    const int e = min(max(top >> 7, 15), 254);        // exponent byte of the largest; q * 2^(134 - e) is below 256
+                    const float up = __uint_as_float(static_cast<uint32_t>(261 - e) << 23);
+                    uint2 hi, lo;
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        const float a = bf16lo(w[2 * k]) * up, b = bf16hi(w[2 * k]) * up, c = bf16lo(w[2 * k + 1]) * up, f = bf16hi(w[2 * k + 1]) * up;
+                        const uint32_t h = e4m3x4(a, b, c, f);
+                        const float2 ab = e4m3x2_value(h & 0xffff), cf = e4m3x2_value(h >> 16);
+                        const uint32_t l = e4m3x4(a - ab.x, b - ab.y, c - cf.x, f - cf.y);
+                        (k ? hi.y : hi.x) = h;
+                        (k ? lo.y : lo.x) = l;
+                    }
+                    // rows of 128 bytes, 16-byte pieces exchanged by the row's number in its group of eight
+                    auto put = [&](uint8_t* tile, int byte, const uint2& v) {
+                        *reinterpret_cast<uint2*>(tile + r * 128 + (((byte >> 4) ^ (r & 7)) << 4) + (byte & 8)) = v;
+                    };
+                    put(q_tile, part * 8, hi);
+                    if (D == 128) put(q_tile + kM * 128, part * 8, lo);
+                    else put(q_tile, 64 + part * 8, lo);
+                    if (part == 0) misc->q_factor[x][r] = top >= 0x7f80 ? __uint_as_float(0x7fffffffu) : __uint_as_float(static_cast<uint32_t>(e - 7) << 23);
+                }
+            }
+            fence_async_smem();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&misc->q_full[x]);
+            // ---- V tiles ----
+            const int ns = u.nt - u.np;
+            for (int t = 0; t < u.nt; ++t, ++tiles) {
+                const int sc = tiles % C::NC, sv = tiles % C::NV;
+                const bool own = t < ns;
+                const int rows = min(kN, own ? u.stot - t * kN : u.key_count - (t - ns) * kN);       // what lies behind is zero
+                const uint8_t* src = c_ring + sc * C::KV_BYTES;
+                uint8_t* dst = v_ring + sv * C::WIDE_BYTES;
+                ok = mbar_wait_warp(&misc->c_full[x][sc], (tiles / C::NC) & 1, misc);
+                if (!ok) break;
+                ok = mbar_wait_warp(&misc->v_empty[x][sv], ((tiles / C::NV) & 1) ^ 1, misc);
+                if (!ok) break;
+                constexpr int PIECES = D / 8;             // of a row: 8 codes each
+#pragma unroll 4
+                for (int i = 0; i < kN * PIECES / 64; ++i) {
+                    const int row = (i * 64 + tid) / PIECES, c = tid % PIECES;
+                    uint2 w = *reinterpret_cast<const uint2*>(src + row * D + c * 8);
+                    if (row >= rows) w = make_uint2(0u, 0u);
+                    if (own) {
+                        // A NaN code must not meet the zero probabilities of other branches' rows: it becomes zero, its branch is noted.  (What
+                        // lies between branches, stale, is no branch's.)
+                        const uint32_t n0 = ((w.x & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u, n1 = ((w.y & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
+                        unsigned hit = __ballot_sync(0xffffffffu, (n0 | n1) != 0);
+                        if (hit) {
+                            w.x &= ~((n0 >> 7) * 0xffu); w.y &= ~((n1 >> 7) * 0xffu);
+                            for (; hit; hit &= hit - 1) {
+                                const int col = t * kN + (i * 64 + half * 32 + __ffs(hit) - 1) / PIECES;
+#pragma unroll
+                                for (int r = 0; r < kRounds; ++r) {
+                                    const bool in = static_cast<uint32_t>(col - static_cast<int>(cols[r] & 0xffff)) < cols[r] >> 16;
+                                    const unsigned who = __ballot_sync(0xffffffffu, in);
+                                    if (lane == 0) misc->nan_branch[x][qc & 1][half][r] |= who;
+                                }
+                            }
+                        }
+                    }
+                    uint4 v;
+                    uint32_t* o = reinterpret_cast<uint32_t*>(&v);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2(static_cast<__nv_fp8x2_storage_t>((k < 2 ? w.x : w.y) >> (k & 1) * 16), __NV_E4M3);
+                        o[k] = static_cast<uint32_t>(h.x) | static_cast<uint32_t>(h.y) << 16;
+                    }
+                    *reinterpret_cast<uint4*>(dst + (c >> 3) * kVHalf + row * 128 + (((c & 7) ^ (row & 7)) << 4)) = v;
+                }
+                fence_async_smem();
+                __syncwarp();
+                if (lane == 0) { mbar_arrive(&misc->v_full[x][sv]); mbar_arrive(&misc->c_empty[x][sc]); }
+            }
+            ++qc;
+        }
     } else {
-        const int64_t ph = static_cast<int64_t>(page) * Hkv + kh;
-        for (int t = 0; t < n; ++t) {
-            const int64_t at = (ph * p.a.g.suffix_cap + t) * D;
-            bool nan = false;
-            for (int e = 0; e < E; ++e) nan |= (p.branch_v[at + lane * E + e] & 0x7f) == 0x7f;
-            bad |= __any_sync(0xffffffffu, nan) != 0;
-            token(p.branch_k + at, p.branch_v + at, e8m0_value(p.branch_scale_k[ph]), e8m0_value(p.branch_scale_v[ph]));
+        // ======================================= softmax =======================================
+        reg_alloc<Regs::SOFTMAX>();
+        const int x = warp >= 8 ? 1 : 0;                 // pipeline
+        const int quad = warp & 3;                       // TMEM lane quadrant this warp may access
+        const int row = quad * 32 + lane;                // tile row = TMEM lane
+        const uint32_t lane_base = static_cast<uint32_t>(quad * 32) << 16;
+        const uint32_t tmem_s0 = tmem + lane_base + x * kColPipe + kColS;
+        const uint32_t tmem_o = tmem + lane_base + x * kColPipe + kColO;
+        uint8_t* stg = smem + C::OFF_STAGE + (x * 4 + quad) * 2048;      // this warp's output staging
+        const int b_row = row / G;                       // branch of this row inside the unit
+        const uint32_t g_magic = 0xFFFFFFFFu / static_cast<uint32_t>(G) + 1u;   // floor(r / G) = umulhi(r, g_magic) for r < 2^16, G > 1
+        uint32_t pw = 0, qc = 0;                         // tiles done (S read, P written), units with tiles
+        bool ok = true;
+        for (uint32_t unit_idx = 0; ok; ++unit_idx) {
+            ok = mbar_wait_warp(&misc->desc_full[x], unit_idx & 1, misc);
+            if (!ok) break;
+            const UnitDesc& d = misc->desc[x];
+            const Unit u = read_unit(d);
+            const int my_cs = d.cs[b_row], my_len = d.len[b_row];
+            const float my_k = e8m0_value(d.ks[b_row]), my_e = d.vs[b_row] == 255 ? __uint_as_float(0x7fffffffu) : static_cast<float>(d.vs[b_row] - 127);
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&misc->desc_empty[x]);
+            if (u.nt < 0) break;
+            const int nt = u.nt, ns = nt - u.np;
+            const int nrows = u.nb * G;
+            const bool row_valid = row < nrows;
+            const bool warp_active = quad * 32 < nrows;
+            float q_factor = 0.f;
+            if (nt > 0) {
+                ok = mbar_wait_warp(&misc->q_full[x], qc & 1, misc);
+                if (!ok) break;
+                q_factor = misc->q_factor[x][row] * p.scale_log2;
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&misc->q_empty[x]);
+            }
+            float R = -INFINITY, M = -INFINITY, l = 0.f;
+            const int j_full = ns + u.key_count / kN;    // tiles [ns, j_full): every row sees them whole
+            for (int j = 0; j < nt && ok; ++j) {
+                int lo = 0, hi = kN;
+                bool vis = warp_active, whole = true;
+                if (warp_active && (j < ns || j >= j_full)) {
+                    if (j >= ns) {
+                        hi = u.key_count - (j - ns) * kN;
+                    } else {
+                        const int base = j * kN;
+                        lo = max(0, my_cs - base);
+                        hi = min(kN, my_cs + my_len - base);
+                        if (hi < lo) hi = lo;
+                    }
+                    vis = __any_sync(0xffffffffu, row_valid && hi > lo);
+                    whole = __all_sync(0xffffffffu, lo == 0 && hi == kN);
+                }
+                const int pb = pw & 1;                   // the tile's S / P buffer
+                const uint32_t tmem_s = tmem_s0 + pb * kN;
+                float ksc[4], ev[4];                     // of the tile's parts: factor of the scores, V exponent
+                ok = mbar_wait_warp(&misc->scale_full[x][pw % kScaleSlots], (pw / kScaleSlots) & 1, misc);
+                if (!ok) break;
+                if (j >= ns) {
+                    const float4 a = misc->scale_k[x][pw % kScaleSlots], b = misc->exp_v[x][pw % kScaleSlots];
+                    ksc[0] = a.x; ksc[1] = a.y; ksc[2] = a.z; ksc[3] = a.w;
+                    ev[0] = b.x; ev[1] = b.y; ev[2] = b.z; ev[3] = b.w;
+                } else {
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) { ksc[c] = my_k; ev[c] = my_e; }
+                }
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    ksc[c] *= q_factor;
+                    if (ksc[c] < 1.17549435e-38f) ksc[c] = 1.17549435e-38f;          // not zero: masked scores are -inf (NaN stays)
+                }
+                ok = mbar_wait_warp(&misc->s_full[x][pb], (pw >> 1) & 1, misc);
+                if (!ok) break;
+                tc_fence_after();
+                if (vis) {
+                    uint32_t sv[kN];
+                    tmem_ld32(tmem_s, sv); tmem_ld32(tmem_s + 32, sv + 32);
+                    tmem_ld_wait();
+                    if (!whole) {
+                        const unsigned span = static_cast<unsigned>(hi - lo);
+#pragma unroll
+                        for (int c = 0; c < kN; ++c)
+                            if (static_cast<unsigned>(c - lo) >= span) sv[c] = 0xff800000u;   // -inf
+                    }
+                    float top_s = -INFINITY, top_r = -INFINITY, ms[4];
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        const uint32_t* s = sv + c * kPart;
+                        float a = fmaxf(__uint_as_float(s[0]), __uint_as_float(s[1])), b = fmaxf(__uint_as_float(s[2]), __uint_as_float(s[3]));
+#pragma unroll
+                        for (int k = 4; k < kPart; k += 4) {
+                            a = fmax3(a, __uint_as_float(s[k]), __uint_as_float(s[k + 1]));
+                            b = fmax3(b, __uint_as_float(s[k + 2]), __uint_as_float(s[k + 3]));
+                        }
+                        ms[c] = fmaxf(a, b) * ksc[c];
+                        top_s = fmaxf(top_s, ms[c]);
+                        top_r = fmaxf(top_r, ms[c] + ev[c]);
+                    }
+                    const float m_new = fmaxf(M, top_s);
+                    if (m_new > M && M != -INFINITY) l *= ex2(M - m_new);
+                    M = m_new;
+                    {
+                        const bool fresh = R == -INFINITY;       // nothing visible so far: O row is still exactly zero
+                        if (fresh) R = top_r;
+                        const bool grow = !fresh && top_r > R + kRescaleSlack;
+                        if (__any_sync(0xffffffffu, grow)) {
+                            // O must be rescaled: wait until the previous P V product has landed in TMEM.  (In a unit's first tile all rows are fresh.)
+                            ok = mbar_wait_warp(&misc->p_empty[x][(pw - 1) & 1], ((pw - 1) >> 1) & 1, misc);
+                            if (ok) {
+                                tc_fence_after();
+                                const float r_new = grow ? top_r : R;
+                                const float f = grow ? ex2(R - r_new) : 1.f;
+#pragma unroll 1
+                                for (int c0 = 0; c0 < D; c0 += 32) {
+                                    uint32_t ov[32];
+                                    tmem_ld32(tmem_o + c0, ov);
+                                    tmem_ld_wait();
+#pragma unroll
+                                    for (int c = 0; c < 32; ++c) ov[c] = __float_as_uint(__uint_as_float(ov[c]) * f);
+                                    tmem_st32(tmem_o + c0, ov);
+                                }
+                                tmem_st_wait();
+                                R = r_new;
+                            }
+                        }
+                    }
+                    if (!ok) break;
+                    // Probabilities go to tensor memory as fp16 pairs, over the first half of the row's own scores.
+                    const float ref = R == -INFINITY ? 0.f : R, sum_ref = (M == -INFINITY ? 0.f : M) + kUp;
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {        // 32 keys = 16 columns of pairs per store
+                        uint32_t pk[16];
+#pragma unroll
+                        for (int c2 = 0; c2 < 2; ++c2) {
+                            const int c = 2 * h + c2;
+                            const float e = fminf(fmaxf(ev[c], ref - kFaint - ms[c]), 400.f) - ref + (ev[c] - ev[c]);       // NaN stays
+                            const uint64_t k2 = pair(ksc[c], ksc[c]), e2 = pair(e + kUp, e + kUp);
+                            uint64_t sum = pair(0.f, 0.f);
+#pragma unroll
+                            for (int k = 0; k < kPart / 2; ++k) {
+                                const uint64_t y = fma2(pair(__uint_as_float(sv[c * kPart + 2 * k]), __uint_as_float(sv[c * kPart + 2 * k + 1])), k2, e2);
+                                float y0, y1;
+                                unpair(y, y0, y1);
+                                const float e0 = ex2(y0), e1 = ex2(y1);
+                                sum = add2(sum, pair(e0, e1));
+                                const __half2 two = __floats2half2_rn(e0, e1);
+                                pk[c2 * 8 + k] = *reinterpret_cast<const uint32_t*>(&two);
+                            }
+                            float a0, a1;
+                            unpair(sum, a0, a1);
+                            l = fmaf(a0 + a1, ex2(-e - sum_ref), l);
+                        }
+                        tmem_st16(tmem_s + h * 16, pk);
+                    }
+                    tmem_st_wait();
+                } else if (warp_active) {                // nothing visible for any row of the warp: zero probabilities
+                    uint32_t pk[16];
+#pragma unroll
+                    for (int c = 0; c < 16; ++c) pk[c] = 0u;
+                    tmem_st16(tmem_s, pk);
+                    tmem_st16(tmem_s + 16, pk);
+                    tmem_st_wait();
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&misc->p_full[x][pb]);
+                ++pw;
+            }
+            if (!ok) break;
+
+            // ------------------------------------ epilogue ------------------------------------
+            if (nt > 0) {                                // the unit's last P V product has landed (and the P tile is free)
+                ok = mbar_wait_warp(&misc->o_full[x], qc & 1, misc);
+                if (!ok) break;
+                const volatile uint32_t* nan = &misc->nan_branch[x][qc & 1][0][0];
+                if (ns > 0 && (nan[b_row >> 5] | nan[4 + (b_row >> 5)]) >> (b_row & 31) & 1) l = __uint_as_float(0x7fffffffu);
+                ++qc;
+            }
+            tc_fence_after();
+            const int g_row = row - b_row * G;
+            const int grow_row = u.row0 + b_row;
+            const int hq = u.head * G + g_row;
+            const bool store = row_valid && grow_row < p.a.a.max_rows;
+            const bool final_out = u.part_base < 0;
+            // o = O 2^(R - 7 - M) / l, the power in two steps: it may be that of any V scale; a partial result leaves the division out
+            const float two = R == -INFINITY ? 0.f : ex2(0.5f * (R - kUp - M));
+            const float inv = two * (l == 0.f ? 0.f : final_out || l != l ? 1.f / l : 1.f);
+            const int64_t pr = (static_cast<int64_t>(final_out ? 0 : u.part_base) + u.row_begin + b_row) * p.a.a.g.Hq + hq;
+            float* po = p.part_o + pr * D;
+            // the accumulator, 32 columns at a time; rolled: the code runs once per unit, out of a cold instruction cache
+            auto read_o = [&](int c0, float (&acc)[32]) {
+                if (warp_active && nt > 0) {
+                    uint32_t ov[32];
+                    tmem_ld32(tmem_o + c0, ov);
+                    tmem_ld_wait();
+#pragma unroll
+                    for (int c = 0; c < 32; ++c) acc[c] = two * __uint_as_float(ov[c]) * inv;
+                } else {
+#pragma unroll
+                    for (int c = 0; c < 32; ++c) acc[c] = 0.f;
+                }
+                if (c0 + 32 >= D && nt > 0) {            // all TMEM reads of this unit are done
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&misc->o_free[x]);
+                }
+            };
+            if (final_out) {
+#pragma unroll 1
+                for (int c0 = 0; c0 < D; c0 += 32) {
+                    float acc[32];
+                    read_o(c0, acc);
+                    // transpose through this warp's 2 KB of shared memory: a row's 32 columns go out as one 64-byte
+                    // piece, 8 rows per store instruction
+#pragma unroll
+                    for (int c = 0; c < 32; c += 8) {
+                        uint4 pk;
+                        pk.x = pack_bf16(acc[c + 0], acc[c + 1]);
+                        pk.y = pack_bf16(acc[c + 2], acc[c + 3]);
+                        pk.z = pack_bf16(acc[c + 4], acc[c + 5]);
+                        pk.w = pack_bf16(acc[c + 6], acc[c + 7]);
+                        *reinterpret_cast<uint4*>(stg + lane * 64 + ((((c >> 3) ^ (lane >> 1)) & 3) << 4)) = pk;
+                    }
+                    __syncwarp();
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int rl = 8 * i + (lane >> 2), ch = lane & 3;       // row inside the warp's 32, 16-byte piece
+                        const uint4 pk = *reinterpret_cast<const uint4*>(stg + rl * 64 + (((ch ^ (rl >> 1)) & 3) << 4));
+                        const int trow = quad * 32 + rl;
+                        const int tb = G == 1 ? trow : static_cast<int>(__umulhi(static_cast<uint32_t>(trow), g_magic)), tg = trow - tb * G;
+                        const int grow = u.row0 + tb;
+                        if (trow < nrows && grow < p.a.a.max_rows)
+                            *reinterpret_cast<uint4*>(p.a.a.o + (static_cast<int64_t>(grow) * p.a.a.g.Hq + u.head * G + tg) * D + c0 + ch * 8) = pk;
+                    }
+                    __syncwarp();
+                }
+            } else {
+#pragma unroll 1
+                for (int c0 = 0; c0 < D; c0 += 32) {
+                    float acc[32];
+                    read_o(c0, acc);
+                    if (store) {
+#pragma unroll
+                        for (int c = 0; c < 32; c += 4)
+                            *reinterpret_cast<float4*>(po + c0 + c) = make_float4(acc[c], acc[c + 1], acc[c + 2], acc[c + 3]);
+                    }
+                }
+            }
+            if (store) {
+                if (final_out) {
+                    if (p.a.a.lse) p.a.a.lse[static_cast<int64_t>(grow_row) * p.a.a.g.Hq + hq] = l == 0.f ? -INFINITY : (M + log2f(l)) * kLn2;
+                } else {
+                    p.part_ml[pr * 2] = M; p.part_ml[pr * 2 + 1] = l;
+                }
+            }
         }
     }
-    if (status && lane == 0 && p.a.dev_status) atomicOr(p.a.dev_status, status);
-    for (int e = 0; e < E; ++e) p.a.o[w * D + lane * E + e] = __float2bfloat16(bad ? NAN : l > 0.f || l != l ? acc[e] / l : 0.f);
-    if (p.a.lse && lane == 0) p.a.lse[w] = bad ? NAN : l > 0.f || l != l ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
+
+    // ---------------------------------------- teardown ----------------------------------------
+    __syncwarp();
+    tc_fence_before();
+    __syncthreads();
+    if (misc->abort_flag) {
+        if (threadIdx.x == 0 && status) atomicOr(status, HPD_S_TIMEOUT);
+        // give copies that may still be in flight time to land before the shared memory is released
+        const long long t0 = clock64();
+        while (clock64() - t0 < 20000000ll) { }
+        __syncthreads();
+    }
+    if (warp == 1) {
+        tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
+    }
+}
+
+// codes [rows, D]: boxes of box_rows rows, swizzled in rows of D bytes
+bool make_codes_map(CUtensorMap* m, const void* base, int D, long long rows, int box_rows)
+{
+    auto fn = tensor_map_encoder();
+    if (!fn) return false;
+    cuuint64_t dims[2] = {static_cast<cuuint64_t>(D), static_cast<cuuint64_t>(rows)};
+    cuuint64_t strides[1] = {static_cast<cuuint64_t>(D)};
+    cuuint32_t box[2] = {static_cast<cuuint32_t>(D), static_cast<cuuint32_t>(box_rows)};
+    cuuint32_t es[2] = {1, 1};
+    return fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              D == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int D>
+int launch_d(const PagedArgs& a)
+{
+    using C = Cfg<D>;
+    // the dynamic shared-memory limit is an attribute of the kernel on ONE device: set it once per device
+    static std::atomic<bool> attr_set[kMaxDevices];
+    const int dev = current_device();
+    if (dev < 0 || dev >= kMaxDevices || !attr_set[dev].load(std::memory_order_acquire)) {
+        HPD_CUDA_TRY(cudaFuncSetAttribute(attn_paged_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM));
+        if (dev >= 0 && dev < kMaxDevices) attr_set[dev].store(true, std::memory_order_release);
+    }
+    const hpd_geom& g = a.a.g;
+    // an empty pool's map still needs an address: any will do, nothing is fetched through it
+    const long long page_rows = static_cast<long long>(a.n_pages) * g.Hkv * a.page_size, branch_rows = static_cast<long long>(a.n_branch_pages) * g.Hkv * g.suffix_cap;
+    const void* pages = page_rows > 0 ? static_cast<const void*>(a.page_k) : a.a.q;
+    const void* branches = branch_rows > 0 ? static_cast<const void*>(a.branch_k) : a.a.q;
+    Maps maps;
+    bool ok = make_codes_map(&maps.page, pages, D, std::max(page_rows, 1ll), a.page_size);
+    for (int i = 0; i < 16 && ok; ++i) ok = make_codes_map(&maps.branch[i], branches, D, std::max(branch_rows, 1ll), i + 1);
+    if (!ok) {
+        set_last_cuda_error(cudaErrorInvalidValue);
+        return HPD_E_CUDA;
+    }
+    Params p{};
+    p.a = a;
+    char* ws = static_cast<char*>(a.a.workspace);
+    p.hdr = reinterpret_cast<const WsHeader*>(ws);
+    p.work = reinterpret_cast<const WorkItem*>(ws + a.a.lay.off_work);
+    p.part_ml = reinterpret_cast<float*>(ws + a.a.lay.off_ml);
+    p.part_o = reinterpret_cast<float*>(ws + a.a.lay.off_o);
+    p.scale_log2 = g.sm_scale * kLog2e;
+    p.G = g.Hq / g.Hkv;
+    attn_paged_kernel<D><<<sm_count(), kThreads, C::SMEM, a.a.stream>>>(maps, p);
+    HPD_CUDA_TRY(cudaGetLastError());
+    return launch_attn_merge(a.a);
 }
 
 }  // namespace
 
-int launch_attn_paged(const PagedArgs& p)
-{
-    const unsigned blocks = static_cast<unsigned>((static_cast<long long>(p.a.max_rows) * p.a.g.Hq + 7) / 8);
-    const float scale = p.a.g.sm_scale * 1.4426950408889634f;
-    if (p.a.g.D == 128) attn_paged_kernel<128><<<blocks, 256, 0, p.a.stream>>>(p, scale);
-    else attn_paged_kernel<64><<<blocks, 256, 0, p.a.stream>>>(p, scale);
-    HPD_CUDA_TRY(cudaGetLastError());
-    return HPD_OK;
-}
+int launch_attn_paged(const PagedArgs& a) { return a.a.g.D == 128 ? launch_d<128>(a) : launch_d<64>(a); }
 
 }  // namespace hpd

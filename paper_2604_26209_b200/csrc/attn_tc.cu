@@ -37,6 +37,7 @@
 #include "common.cuh"
 #include "copy_warps.h"
 #include "ptx.cuh"
+#include "tc.cuh"
 
 namespace hpd {
 
@@ -56,7 +57,6 @@ constexpr int kKHalf = kN * 128;           // one 64-element half of a K or V ti
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kRescaleSlack = 8.0f;      // tolerated growth of the row maximum (log2 units) before O is rescaled
-constexpr long long kWaitCycles = 4000000000ll;   // ~2 s at 2 GHz
 // TMEM columns of one pipeline (the second pipeline's start 256 columns further): two score tiles of 64 columns (the
 // probabilities of a tile, bf16 pairs, overwrite the first 32 columns of its scores) and the output accumulator
 constexpr uint32_t kColPipe = 256, kColS = 0, kColO = 128;
@@ -142,98 +142,8 @@ struct Misc {
 static_assert(sizeof(Misc) <= 5120, "misc block");
 
 // ------------------------------------------------------------------------------------------------
-// PTX wrappers
+// tensor-core operands
 // ------------------------------------------------------------------------------------------------
-// Bounded wait.  Returns false after ~2 s or once another thread of the CTA has given up.
-__device__ __forceinline__ bool mbar_wait(unsigned long long* bar, uint32_t parity, Misc* misc) {
-    if (mbar_try_wait(bar, parity)) return true;
-    const long long t0 = clock64();
-    int spins = 0;
-    while (!mbar_try_wait(bar, parity)) {
-        if ((++spins & 1023) == 0) {
-            if (*reinterpret_cast<volatile int*>(&misc->abort_flag)) return false;
-            if (clock64() - t0 > kWaitCycles) {
-                *reinterpret_cast<volatile int*>(&misc->abort_flag) = 1;
-                return false;
-            }
-        }
-    }
-    return true;
-}
-
-// all lanes wait; the result is made warp-uniform so that warp-collective instructions stay converged
-__device__ __forceinline__ bool mbar_wait_warp(unsigned long long* bar, uint32_t parity, Misc* misc) {
-    return __all_sync(0xffffffffu, mbar_wait(bar, parity, misc));
-}
-
-// One lane of the converged warp.  Measured against lane == 0: issuing eight tensor-core instructions ~300 cycles instead of ~1200,
-// attention of 64 prompts 156 -> 153 us, first inference step 3.48 -> 3.33 ms.
-__device__ __forceinline__ bool elect_one() {
-    uint32_t p;
-    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
-    return p != 0;
-}
-__device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-
-__device__ __forceinline__ void tc_commit(unsigned long long* bar) {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
-}
-// One tcgen05.mma; the two shared-memory descriptors are given as their low words (address and LBO fields, see
-// below), the high word is the same for every operand of this kernel.
-__device__ __forceinline__ void tc_mma(uint32_t d_tmem, uint32_t a_lo, uint32_t b_lo, uint32_t idesc, uint32_t accumulate) {
-    asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\t"
-                 "mov.b64 da, {%1, %5};\n\tmov.b64 db, {%2, %5};\n\tsetp.ne.b32 p, %4, 0;\n\t"
-                 "tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %3, p;\n\t}"
-                 ::"r"(d_tmem), "r"(a_lo), "r"(b_lo), "r"(idesc), "r"(accumulate), "r"(0x40004040u) : "memory");
-}
-
-// The same with the A operand in tensor memory (the probabilities, written there by the softmax threads).
-__device__ __forceinline__ void tc_mma_ts(uint32_t d_tmem, uint32_t a_tmem, uint32_t b_lo, uint32_t idesc, uint32_t accumulate) {
-    asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 db;\n\t"
-                 "mov.b64 db, {%2, %5};\n\tsetp.ne.b32 p, %4, 0;\n\t"
-                 "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %3, p;\n\t}"
-                 ::"r"(d_tmem), "r"(a_tmem), "r"(b_lo), "r"(idesc), "r"(accumulate), "r"(0x40004040u) : "memory");
-}
-
-#define HPD_R8(a, o) "=r"(a[o + 0]), "=r"(a[o + 1]), "=r"(a[o + 2]), "=r"(a[o + 3]), "=r"(a[o + 4]), "=r"(a[o + 5]), "=r"(a[o + 6]), "=r"(a[o + 7])
-#define HPD_W8(a, o) "r"(a[o + 0]), "r"(a[o + 1]), "r"(a[o + 2]), "r"(a[o + 3]), "r"(a[o + 4]), "r"(a[o + 5]), "r"(a[o + 6]), "r"(a[o + 7])
-// 32 consecutive fp32 columns of this thread's TMEM lane
-__device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t* v) {
-    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
-                 "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
-                 : HPD_R8(v, 0), HPD_R8(v, 8), HPD_R8(v, 16), HPD_R8(v, 24) : "r"(taddr) : "memory");
-}
-__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t* v) {
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,"
-                 "%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};"
-                 ::"r"(taddr), HPD_W8(v, 0), HPD_W8(v, 8), HPD_W8(v, 16), HPD_W8(v, 24) : "memory");
-}
-__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t* v) {
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
-                 ::"r"(taddr), HPD_W8(v, 0), HPD_W8(v, 8) : "memory");
-}
-__device__ __forceinline__ void tmem_ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
-__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-
-__device__ __forceinline__ float ex2(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-// pairs of fp32 in one 64-bit register: two fused multiply-adds or additions per instruction, each rounded as usual
-__device__ __forceinline__ uint64_t pair(float a, float b) { uint64_t r; asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b)); return r; }
-__device__ __forceinline__ void unpair(uint64_t v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
-__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) { uint64_t r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c)); return r; }
-__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) { uint64_t r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
-__device__ __forceinline__ float fmax3(float a, float b, float c) {
-    float d;
-    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
-    return d;
-}
-template <int N> __device__ __forceinline__ void reg_dealloc() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
-template <int N> __device__ __forceinline__ void reg_alloc() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
-
 // Shared-memory matrix descriptors (128-byte swizzle; version field = 1).  High word, common to all operands:
 // SBO = 1024 B (groups of 8 rows), version 1, swizzle mode 2 (128 B) = 0x40004040.  Low word: address / 16 in bits
 // 0-13 and LBO / 16 in bits 16-29.  Shared-memory addresses are below 2^18, so moving a descriptor by a multiple
@@ -1092,7 +1002,7 @@ hpd_merge_kernel(TcParams p, const DocSplit* split)
         } else {
             *reinterpret_cast<uint32_t*>(op) = pack_bf16(acc[0] * inv, acc[1] * inv);
         }
-        if (p.a.lse && lane == 0) p.a.lse[w] = L > 0.f ? (M + log2f(L)) * kLn2 : -INFINITY;
+        if (p.a.lse && lane == 0) p.a.lse[w] = L == 0.f ? -INFINITY : (M + log2f(L)) * kLn2;
     }
 }
 
@@ -1127,6 +1037,35 @@ bool make_q_map(CUtensorMap* m, const void* base, int D, int G, int Hkv, long lo
     return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims, strides, box, es,
               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+TcParams make_params(const AttnArgs& a)
+{
+    TcParams p{};
+    p.a = a;
+    char* ws = static_cast<char*>(a.workspace);
+    p.hdr = reinterpret_cast<const WsHeader*>(ws);
+    p.work = reinterpret_cast<const WorkItem*>(ws + a.lay.off_work);
+    p.part_ml = reinterpret_cast<float*>(ws + a.lay.off_ml);
+    p.part_o = reinterpret_cast<float*>(ws + a.lay.off_o);
+    p.scale_log2 = a.g.sm_scale * kLog2e;
+    p.G = a.g.Hq / a.g.Hkv;
+    return p;
+}
+
+template <int D>
+int launch_merge(const TcParams& p, bool never_split)
+{
+    const AttnArgs& a = p.a;
+    const int n_sm = sm_count();
+    // one warp per (row, q head) where the rows allow it, at most two resident waves (four blocks an SM); with many documents
+    // nothing is split as a rule (the kernel then only rewinds the ticket counter) and a small grid is launched sooner
+    const long long merge_blocks = (static_cast<long long>(a.max_rows) * a.g.Hq + 7) / 8;
+    const long long merge_cap = static_cast<long long>(a.n_docs) * a.g.Hkv < 4ll * n_sm ? 8ll * n_sm : 2ll * n_sm;
+    const int merge_grid = never_split ? 1 : static_cast<int>(std::min<long long>(std::max<long long>(merge_blocks, 1), merge_cap));
+    const DocSplit* split = reinterpret_cast<const DocSplit*>(static_cast<char*>(a.workspace) + a.lay.off_split);
+    HPD_CUDA_TRY(launch_chained(hpd_merge_kernel<D>, merge_grid, 256, 0, a.stream, p, split));
+    return HPD_OK;
 }
 
 template <int D, int MODE>
@@ -1179,15 +1118,7 @@ int launch_d(const AttnArgs& a)
     }
     const CUtensorMap &mq = ms->mq, &mk = ms->mk, &mv = ms->mv;
     const SufMaps& sm = ms->sm;
-    TcParams p{};
-    p.a = a;
-    char* ws = static_cast<char*>(a.workspace);
-    p.hdr = reinterpret_cast<const WsHeader*>(ws);
-    p.work = reinterpret_cast<const WorkItem*>(ws + a.lay.off_work);
-    p.part_ml = reinterpret_cast<float*>(ws + a.lay.off_ml);
-    p.part_o = reinterpret_cast<float*>(ws + a.lay.off_o);
-    p.scale_log2 = a.g.sm_scale * kLog2e;
-    p.G = G;
+    const TcParams p = make_params(a);
     const int n_sm = sm_count();
     CUtensorMap mbk = mk, mbv = mv;                      // unused without a shared block
     if constexpr (MODE == kBlock) {
@@ -1197,17 +1128,18 @@ int launch_d(const AttnArgs& a)
         }
     }
     HPD_CUDA_TRY(launch_chained(hpd_attn_tc_kernel<D, MODE>, n_sm, kThreadsOf<MODE>, C::SMEM, a.stream, mq, mk, mv, mbk, mbv, sm, p));
-    // one warp per (row, q head) where the rows allow it, at most two resident waves (four blocks an SM); with many documents
-    // nothing is split as a rule (the kernel then only rewinds the ticket counter) and a small grid is launched sooner
-    const long long merge_blocks = (static_cast<long long>(a.max_rows) * a.g.Hq + 7) / 8;
-    const long long merge_cap = static_cast<long long>(a.n_docs) * a.g.Hkv < 4ll * n_sm ? 8ll * n_sm : 2ll * n_sm;
-    const int merge_grid = MODE == kPrefill ? 1          // never split
-                         : static_cast<int>(std::min<long long>(std::max<long long>(merge_blocks, 1), merge_cap));
-    HPD_CUDA_TRY(launch_chained(hpd_merge_kernel<D>, merge_grid, 256, 0, a.stream, p, reinterpret_cast<const DocSplit*>(ws + a.lay.off_split)));
-    return HPD_OK;
+    return launch_merge<D>(p, MODE == kPrefill);
+}
+
+template <int D>
+int launch_split_merge(const AttnArgs& a)
+{
+    return launch_merge<D>(make_params(a), false);
 }
 
 }  // namespace
+
+int launch_attn_merge(const AttnArgs& a) { return a.g.D == 128 ? launch_split_merge<128>(a) : launch_split_merge<64>(a); }
 
 int launch_attn_tc(const AttnArgs& a)
 {
