@@ -46,33 +46,33 @@ constexpr float kRescaleSlack = 8.0f;      // tolerated growth of the reference 
 constexpr float kUp = 7.0f;                // probabilities are 2^7 larger: 2^15 at most, fp16 holds 65504
 constexpr float kFaint = 60.0f;            // products below 2^-60 of the reference are dropped
 constexpr uint32_t kColPipe = 256, kColS = 0, kColO = 128;
-struct Regs { static constexpr int IO = 112, SOFTMAX = 168, CONVERT = 64; };
+struct Regs { static constexpr int IO = 104, SOFTMAX = 160, CONVERT = 88; };
 static_assert(Regs::IO + 2 * Regs::SOFTMAX + Regs::CONVERT <= 4 * 128, "registers traded between the warpgroups exceed the CTA's allocation");
 constexpr int kRounds = 4;                 // a unit has at most 128 branches: 4 rounds of 32 lanes
 constexpr int kDescReaders = 7;            // MMA thread, four softmax warps, two conversion warps
-constexpr int kScaleSlots = 8;             // tiles whose scales are kept: more than the copies can run ahead of the softmax
 
 template <int D> struct Cfg {
     static constexpr int Q_BYTES = kM * 2 * D;                   // two e4m3 terms of every element
     static constexpr int KV_BYTES = kN * D;                      // one tile of codes
     static constexpr int WIDE_BYTES = kN * 2 * D;                // one V tile in fp16
-    static constexpr int NK = D == 128 ? 3 : 4;                  // K stages of a pipeline
-    static constexpr int NC = D == 128 ? 3 : 4;                  // V stages as codes
+    static constexpr int NK = D == 128 ? 3 : 4;                               // K stages of a pipeline
+    static constexpr int NC = 4;                  // V stages as codes
     static constexpr int NV = D == 128 ? 1 : 2;                  // V stages in fp16
     static constexpr int PAD = D == 128 ? 1 : 2;                 // a branch begins at a multiple of PAD columns (a copy's destination: 128 bytes)
     static constexpr int OFF_Q = 0;
-    static constexpr int OFF_STAGE = OFF_Q + 2 * Q_BYTES;        // output transpose, 2 KB per softmax warp
-    static constexpr int OFF_K = OFF_STAGE + 8 * 2048;
+    static constexpr int OFF_STAGE = OFF_Q + 2 * Q_BYTES;        // output transpose, 1 KB per softmax warp
+    static constexpr int OFF_K = OFF_STAGE + 8 * 1024;
     static constexpr int OFF_C = OFF_K + 2 * NK * KV_BYTES;
     static constexpr int OFF_V = OFF_C + 2 * NC * KV_BYTES;
     static constexpr int OFF_MISC = OFF_V + 2 * NV * WIDE_BYTES;
     static constexpr int SMEM = OFF_MISC + 6144;
     static_assert(OFF_V % 1024 == 0 && OFF_K % 1024 == 0, "swizzled tiles");
-    static_assert(NK + 2 < kScaleSlots, "scales are kept until the softmax has used them");
+    static_assert(NK + 2 < 8, "a batch of pages has at least eight tiles");
 };
 static_assert(Cfg<128>::SMEM <= 232448, "shared memory budget");
 
 struct Maps {
+    CUtensorMap q;                         // bf16: boxes of 128/G rows x G heads x 64 elements
     CUtensorMap page;                      // K codes of the documents: boxes of one page
     CUtensorMap branch[16];                // K codes of the branches: boxes of 1 .. 16 tokens
 };
@@ -91,7 +91,8 @@ struct UnitDesc {
     int np;                                // document's tiles
     int stot;                              // packed columns of the branches
     int head, key_count, part_base, row_begin, nb /*branches*/, row0 /*first global row*/;
-    int pad[7];
+    int nb_cached;                         // branches whose tokens the unit visits: entries below
+    int pad[6];
     uint16_t cs[kM];                       // per branch: packed column of its first token
     uint16_t len[kM];                      // per branch: tokens visible
     uint8_t ks[kM], vs[kM];                // per branch: scale bytes of its page
@@ -100,19 +101,31 @@ static_assert(sizeof(UnitDesc) == 64 + 6 * kM, "descriptor size");
 
 constexpr int kMaxStages = 4;
 struct Misc {
-    unsigned long long q_full[2], q_empty[2];
-    unsigned long long k_full[2][kMaxStages], k_empty[2][kMaxStages], c_full[2][kMaxStages], c_empty[2][kMaxStages], v_full[2][kMaxStages], v_empty[2][kMaxStages];
-    unsigned long long s_full[2][2], p_full[2][2], p_empty[2][2], o_full[2], o_free[2];
-    unsigned long long desc_full[2], desc_empty[2], scale_full[2][kScaleSlots];
+    unsigned long long q_raw[2], q_full[2], q_empty[2];          // q as it is has come; its two terms are there; the tile is free
+    unsigned long long k_full[2][kMaxStages], k_empty[2][kMaxStages], c_full[2][kMaxStages], c_empty[2][kMaxStages], v_empty[2][kMaxStages];
+    unsigned long long s_full[2][2], pv_full[2][2], o_full[2], o_free[2];        // pv: the probabilities and the widened V tile
+    unsigned long long desc_full[2], desc_empty[2], batch_full[2];
     uint32_t tmem_base;
     int abort_flag;
     int pad[2];
-    float4 scale_k[2][kScaleSlots], exp_v[2][kScaleSlots];       // of a document's tile: K scale and V exponent of every 16 columns
+    float2 page_scale[2][2][64];           // pipeline, unit's parity: K scale and V exponent of the document's pages, two batches of 32
     float q_factor[2][kM];                 // what the scaled rows of q have to be multiplied by
     uint32_t nan_branch[2][2][2][4];       // pipeline, unit's parity, conversion warp: branches with a NaN among their values
     UnitDesc desc[2];
 };
 static_assert(sizeof(Misc) <= 6144, "misc block");
+
+// Bounded wait: false once two to four seconds (2^32 cycles and more) have passed or another thread of the CTA has given up.  Short on purpose: it stands
+// at some forty places, and the kernel's code competes for the instruction cache (138 KB of it cost 8 % against 80).
+__device__ __forceinline__ uint32_t clock_high() { uint32_t t; asm volatile("mov.u32 %0, %%clock_hi;" : "=r"(t)); return t; }
+__device__ __forceinline__ bool wait_for(unsigned long long* bar, uint32_t parity, Misc* misc) {
+    if (mbar_try_wait(bar, parity)) return true;
+    return mbar_wait(bar, parity, misc);
+}
+// all lanes wait; the result is made warp-uniform so that warp-collective instructions stay converged
+__device__ __forceinline__ bool wait_for_warp(unsigned long long* bar, uint32_t parity, Misc* misc) {
+    return __all_sync(0xffffffffu, wait_for(bar, parity, misc));
+}
 
 // tcgen05.mma on two operands of e4m3 codes in shared memory (descriptors' low and high words)
 __device__ __forceinline__ void tc_mma_codes(uint32_t d_tmem, uint32_t a_lo, uint32_t a_hi, uint32_t b_lo, uint32_t b_hi, uint32_t idesc, uint32_t accumulate) {
@@ -142,7 +155,7 @@ attn_paged_kernel(const __grid_constant__ Maps maps, const Params p)
     extern __shared__ __align__(1024) uint8_t smem[];
     Misc* misc = reinterpret_cast<Misc*>(smem + C::OFF_MISC);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int G = p.G, Hkv = p.a.a.g.Hkv;
+    const int G = p.G, g_shift = 31 - __clz(G), Hkv = p.a.a.g.Hkv;       // G: 1, 2, 4 or 8
     int32_t* status = p.a.a.dev_status;
     if ((smem_u32(smem) & 1023u) != 0) {                 // swizzled tiles need 1024-byte alignment: refuse rather than misread
         if (threadIdx.x == 0 && status) atomicOr(status, HPD_S_BAD_TABLE);
@@ -150,16 +163,16 @@ attn_paged_kernel(const __grid_constant__ Maps maps, const Params p)
     }
     if (threadIdx.x == 0) {
         for (int i = 0; i < 2; ++i) {
-            mbar_init(&misc->q_full[i], 2);  mbar_init(&misc->q_empty[i], 5);
-            for (int b = 0; b < 2; ++b) { mbar_init(&misc->s_full[i][b], 1); mbar_init(&misc->p_full[i][b], 4); mbar_init(&misc->p_empty[i][b], 1); }
+            mbar_init(&misc->q_raw[i], 1);   mbar_init(&misc->q_full[i], 2);  mbar_init(&misc->q_empty[i], 5);
+            for (int b = 0; b < 2; ++b) { mbar_init(&misc->s_full[i][b], 1); mbar_init(&misc->pv_full[i][b], 6); }
             mbar_init(&misc->o_full[i], 1);  mbar_init(&misc->o_free[i], 4);
             mbar_init(&misc->desc_full[i], 1); mbar_init(&misc->desc_empty[i], kDescReaders);
             for (int k = 0; k < kMaxStages; ++k) {
                 mbar_init(&misc->k_full[i][k], 1); mbar_init(&misc->k_empty[i][k], 1);
                 mbar_init(&misc->c_full[i][k], 1); mbar_init(&misc->c_empty[i][k], 2);
-                mbar_init(&misc->v_full[i][k], 2); mbar_init(&misc->v_empty[i][k], 1);
+                mbar_init(&misc->v_empty[i][k], 1);
             }
-            for (int k = 0; k < kScaleSlots; ++k) mbar_init(&misc->scale_full[i][k], 1);
+            mbar_init(&misc->batch_full[i], 1);
         }
         misc->abort_flag = 0;
         fence_mbar_init();
@@ -180,14 +193,18 @@ attn_paged_kernel(const __grid_constant__ Maps maps, const Params p)
     if (warp == 0 || warp == 3) {
         // ============================ scheduler and copies of one pipeline =====================
         // Units are drawn as in hpd_attn_decode: six fixed ones per pipeline, then from the step's ticket counter.  What a unit needs to
-        // know is a chain of loads -- item, row tables, pages, scales -- of which the unit before issues one link at a time between
-        // its tiles.
+        // know is a chain of loads -- item, row tables, pages, scales -- of which the unit before issues one link after another between
+        // its first tiles.
         reg_dealloc<Regs::IO>();
         const int x = warp == 0 ? 0 : 1;
+        // The pipeline's first item is one of two, whichever way the units are laid over the SMs: both are asked for together with the header.
+        const int first_spread = blockIdx.x + x * gridDim.x, first_pair = 2 * blockIdx.x + x;
+        const WorkItem it_spread = p.work[min(first_spread / Hkv, p.a.a.lay.work_cap - 1)];
+        const WorkItem it_pair = p.work[min(first_pair / Hkv, p.a.a.lay.work_cap - 1)];
         const int n_units = p.hdr->n_work * Hkv;
+        const bool alternate = p.hdr->longest_first != 0;
         const int P = p.a.page_size, shift = 31 - __clz(P);          // tokens of a page: 2^shift
-        const int per_tile = kN >> shift;                            // pages of a tile
-        const int per_batch = 32 / per_tile;                         // tiles whose pages the lanes hold
+        const int per_tile = kN >> shift, per_batch = 32 / per_tile; // pages of a tile; tiles whose pages the lanes hold (8, 16 or 32)
         uint32_t* ticket = const_cast<uint32_t*>(&p.hdr->ticket);
         UnitDesc& d = misc->desc[x];
         uint8_t* k_ring = smem + C::OFF_K + x * C::NK * C::KV_BYTES;
@@ -196,7 +213,6 @@ attn_paged_kernel(const __grid_constant__ Maps maps, const Params p)
             if (lane == 0) { d.nt = -1; mbar_arrive(&misc->desc_full[x]); }
         } else {
         constexpr int kStatic = 6;
-        const bool alternate = p.hdr->longest_first != 0;
         const bool spread = n_units < 4 * 2 * static_cast<int>(gridDim.x);
         const uint32_t first_dynamic = static_cast<uint32_t>(kStatic) * 2u * gridDim.x;
         auto next = [&](int i) {                                     // the pipeline's i-th unit
@@ -213,9 +229,10 @@ attn_paged_kernel(const __grid_constant__ Maps maps, const Params p)
         auto item_of = [&](int w) { return p.work[min(w, n_units - 1) / Hkv]; };
         // ---- the links of a unit's chain: row tables and page numbers; branches' pages; scales ----
         int len[kRounds], page[kRounds], ks[kRounds], vs[kRounds];   // per branch; page: slot, then page, then first row of its codes
-        int doc_row, bad;                                            // first row of the document; a table entry out of range
+        int bad;                                                     // a table entry out of range
         // per lane: one of 32 pages of the document: its number (-2: not needed), then first row of its codes (-1: none) and scale bytes
         int id, row, sk, sv;
+        auto branches_of = [&](int w, const WorkItem& it) { return w < n_units && it.with_suffix ? it.row_count : 0; };
         auto page_id = [&](const WorkItem& it, int i) {
             const int at = (it.key_begin >> shift) + i;
             if (i << shift >= it.key_count) return -2;
@@ -229,14 +246,15 @@ attn_paged_kernel(const __grid_constant__ Maps maps, const Params p)
             row_ = static_cast<int>(ph << shift);
             sk_ = p.a.scale_k[ph]; sv_ = p.a.scale_v[ph];
         };
-        auto link_rows = [&](int w, const WorkItem& it, int das) {
+        auto link_rows = [&](int w, const WorkItem& it) {
+            const int nb = branches_of(w, it);
 #pragma unroll
             for (int r = 0; r < kRounds; ++r) {
                 const int b = lane + 32 * r;
                 len[r] = 0; page[r] = -1;
-                if (w < n_units && it.with_suffix && b < it.row_count) {
-                    len[r] = p.a.a.suffix_len[das + it.row_begin + b];
-                    page[r] = p.a.a.active_slot[das + it.row_begin + b];
+                if (b < nb) {
+                    len[r] = p.a.a.suffix_len[it.doc_row + it.row_begin + b];
+                    page[r] = p.a.a.active_slot[it.doc_row + it.row_begin + b];
                 }
             }
             id = w < n_units ? page_id(it, lane) : -2;
@@ -268,143 +286,135 @@ attn_paged_kernel(const __grid_constant__ Maps maps, const Params p)
             }
             page_scales(id, head, row, sk, sv);
         };
-        int w0 = next(0), w1 = next(1);
-        WorkItem it0 = item_of(w0), it1 = item_of(w1);
-        doc_row = it0.doc_row;
-        link_rows(w0, it0, doc_row);
-        link_pages();
-        link_scales(w0);
-        uint32_t kc = 0;                                             // tiles so far
+        auto report = [&]() { if (__any_sync(0xffffffffu, bad) && lane == 0 && status) atomicOr(status, HPD_S_BAD_TABLE); };
+        // unit ui is w0, the next one w1; before the first there is one without tiles, so that the links stand in one place
+        int w0 = n_units, w1 = next(0);
+        WorkItem it0 = it_spread, it1 = (spread ? first_spread : first_pair) < n_units ? (spread ? it_spread : it_pair) : item_of(w1);
+        int st = 0, sc = 0;                                          // stages of the next tile's copies, and the parities of their barriers
+        uint32_t k_par = 1, c_par = 1;
         bool ok = true;
-        for (uint32_t ui = 0; ok; ++ui) {
+        for (int ui = -1; ok; ++ui) {
+            int nt = 0, ns = 0, np = 0, head = 0, row0 = 0, key_count = 0, carry = 0, nb = 0;
+            int cs[kRounds], blen[kRounds], brow[kRounds];           // per branch: first column, tokens, first row of its codes
+            float2* scales = misc->page_scale[x][ui & 1];
+            auto put_scales = [&](int batch, int k, int v) {
+                scales[(batch & 1) * 32 + lane] = make_float2(e8m0_value(k), v == 255 ? __uint_as_float(0x7fffffffu) : static_cast<float>(v - 127));
+            };
+            int cur_row = -1, nxt_id = -2, nxt_row = -1, nxt_sk = 127, nxt_sv = 127;       // this unit's batch of 32 pages, and the next
+            if (ui >= 0) {
             // ---- scan and publish unit ui ----
             if (ui >= 1) {
-                ok = mbar_wait_warp(&misc->desc_empty[x], (ui - 1) & 1, misc);
+                ok = wait_for_warp(&misc->desc_empty[x], (ui - 1) & 1, misc);
                 if (!ok) break;
             }
             const bool live = w0 < n_units;
-            if (__any_sync(0xffffffffu, bad) && lane == 0 && status) atomicOr(status, HPD_S_BAD_TABLE);
-            int cs[kRounds];
-            int carry = 0;
+            report();
+            nb = branches_of(w0, it0);
 #pragma unroll
             for (int r = 0; r < kRounds; ++r) {
-                const int b = lane + 32 * r;
-                const int occ = (len[r] + C::PAD - 1) / C::PAD * C::PAD;
-                int incl = occ;
+                cs[r] = 0; blen[r] = 0; brow[r] = 0;
+                if (32 * r < nb) {
+                    const int b = lane + 32 * r;
+                    const int occ = (len[r] + C::PAD - 1) / C::PAD * C::PAD;
+                    int incl = occ;
 #pragma unroll
-                for (int s = 1; s < 32; s <<= 1) {
-                    const int v = __shfl_up_sync(0xffffffffu, incl, s);
-                    if (lane >= s) incl += v;
+                    for (int s = 1; s < 32; s <<= 1) {
+                        const int v = __shfl_up_sync(0xffffffffu, incl, s);
+                        if (lane >= s) incl += v;
+                    }
+                    cs[r] = carry + incl - occ; blen[r] = len[r]; brow[r] = page[r];
+                    d.cs[b] = static_cast<uint16_t>(cs[r]);
+                    d.len[b] = static_cast<uint16_t>(len[r]);
+                    d.ks[b] = static_cast<uint8_t>(ks[r]);
+                    d.vs[b] = static_cast<uint8_t>(vs[r]);
+                    carry += __shfl_sync(0xffffffffu, incl, 31);
                 }
-                cs[r] = carry + incl - occ;
-                d.cs[b] = static_cast<uint16_t>(cs[r]);
-                d.len[b] = static_cast<uint16_t>(len[r]);
-                d.ks[b] = static_cast<uint8_t>(ks[r]);
-                d.vs[b] = static_cast<uint8_t>(vs[r]);
-                carry += __shfl_sync(0xffffffffu, incl, 31);
             }
-            const int nrounds = ((live && it0.with_suffix ? it0.row_count : 0) + 31) >> 5;
-            const int ns = (carry + kN - 1) / kN, np = live ? (it0.key_count + kN - 1) / kN : 0;
-            const int nt = live ? ns + np : -1, head = w0 % Hkv;
+            ns = (carry + kN - 1) / kN; np = live ? (it0.key_count + kN - 1) / kN : 0;
+            nt = live ? ns + np : -1; head = w0 % Hkv; row0 = it0.doc_row + it0.row_begin; key_count = it0.key_count;
             if (lane == 0) {
-                d.nt = nt; d.np = np; d.stot = carry; d.head = head; d.key_count = it0.key_count; d.part_base = it0.part_base;
-                d.row_begin = it0.row_begin; d.nb = it0.row_count; d.row0 = doc_row + it0.row_begin;
+                d.nt = nt; d.np = np; d.stot = carry; d.head = head; d.key_count = key_count; d.part_base = it0.part_base;
+                d.row_begin = it0.row_begin; d.nb = it0.row_count; d.row0 = row0; d.nb_cached = nb;
             }
+            put_scales(0, sk, sv);
             __syncwarp();
             if (lane == 0) mbar_arrive(&misc->desc_full[x]);
             if (!live) break;
-            // this unit's chain moves out of the way of the next one's
-            int blen[kRounds], brow[kRounds];
-#pragma unroll
-            for (int r = 0; r < kRounds; ++r) { blen[r] = len[r]; brow[r] = page[r]; }
-            int cur_row = row, cur_sk = sk, cur_sv = sv;             // this unit's batch of 32 pages, and the next
-            int nxt_id = page_id(it0, 32 + lane), nxt_row = -1, nxt_sk = 127, nxt_sv = 127;
-            const int w2 = next(static_cast<int>(ui) + 2);
+            if (np > 0 || ns > 0)                                    // q on its way into L2: its tile is released late in the unit before
+                if (elect_one())
+                    for (int h = 0; h < D / 64; ++h) tma_prefetch_4d(&maps.q, h * 64, 0, head, row0);
+            __syncwarp();
+            cur_row = row;
+            nxt_id = page_id(it0, 32 + lane);
+            }
+            const int w2 = next(ui + 2);
             const WorkItem it2 = item_of(w2);
-            doc_row = it1.doc_row;
-            link_rows(w1, it1, doc_row);
-            for (int t = 0; t < nt && ok; ++t, ++kc) {
-                const uint32_t st = kc % C::NK, sc = kc % C::NC, slot = kc % kScaleSlots;
+            link_rows(w1, it1);
+            for (int t = 0; t < max(nt, 2) && ok; ++t) {
+                if (t < nt) {
                 uint8_t* kt = k_ring + st * C::KV_BYTES;
                 uint8_t* ct = c_ring + sc * C::KV_BYTES;
                 unsigned long long *kf = &misc->k_full[x][st], *cf = &misc->c_full[x][sc];
+                ok = wait_for_warp(&misc->k_empty[x][st], k_par, misc) && wait_for_warp(&misc->c_empty[x][sc], c_par, misc);
+                if (!ok) break;
                 if (t < ns) {
                     // pieces of the branches that fall into the tile; a box has the exact height of the piece
                     const int c_lo = t * kN, c_hi = min(carry, c_lo + kN);
                     int mine = 0;
 #pragma unroll
-                    for (int r = 0; r < kRounds; ++r) mine += max(0, min(cs[r] + blen[r], c_hi) - max(cs[r], c_lo));
+                    for (int r = 0; r < kRounds; ++r)
+                        if (32 * r < nb) mine += max(0, min(cs[r] + blen[r], c_hi) - max(cs[r], c_lo));
                     const uint32_t bytes = __reduce_add_sync(0xffffffffu, mine) * D;
-                    ok = mbar_wait_warp(&misc->k_empty[x][st], ((kc / C::NK) & 1) ^ 1, misc);
-                    if (!ok) break;
-                    if (lane == 0) mbar_expect_tx(kf, bytes);
+                    if (lane == 0) { mbar_expect_tx(kf, bytes); mbar_expect_tx(cf, bytes); }
 #pragma unroll
                     for (int r = 0; r < kRounds; ++r) {
-                        if (r >= nrounds) break;
+                        if (32 * r >= nb) break;
                         const int lo = max(cs[r], c_lo);
                         int n = min(cs[r] + blen[r], c_hi) - lo, from = brow[r] + (lo - cs[r]), col = lo - c_lo;
+                        if (n > 0) bulk_load(ct + col * D, p.a.branch_v + static_cast<int64_t>(from) * D, cf, static_cast<uint32_t>(n) * D);
                         while (n > 0) {
                             const int hb = min(n, 16);
                             tma_load_2d(kt + col * D, &maps.branch[hb - 1], kf, 0, from);
                             from += hb; col += hb; n -= hb;
                         }
                     }
-                    if (lane == 0) mbar_arrive(&misc->scale_full[x][slot]);
-                    __syncwarp();
-                    ok = mbar_wait_warp(&misc->c_empty[x][sc], ((kc / C::NC) & 1) ^ 1, misc);
-                    if (!ok) break;
-                    if (lane == 0) mbar_expect_tx(cf, bytes);
-#pragma unroll
-                    for (int r = 0; r < kRounds; ++r) {
-                        if (r >= nrounds) break;
-                        const int lo = max(cs[r], c_lo), n = min(cs[r] + blen[r], c_hi) - lo;
-                        if (n > 0) bulk_load(ct + (lo - c_lo) * D, p.a.branch_v + static_cast<int64_t>(brow[r] + (lo - cs[r])) * D, cf, static_cast<uint32_t>(n) * D);
-                    }
                 } else {
-                    const int tp = t - ns, in_batch = tp % per_batch;
+                    // the lanes that hold the tile's pages copy them
+                    const int tp = t - ns, in_batch = tp & (per_batch - 1);
                     if (tp > 0 && in_batch == 0) {                   // the next 32 pages; ask for the ones behind them
-                        cur_row = nxt_row; cur_sk = nxt_sk; cur_sv = nxt_sv;
+                        cur_row = nxt_row;
                         nxt_id = page_id(it0, (tp / per_batch + 1) * 32 + lane);
                     }
-                    const int pages = (min(kN, it0.key_count - tp * kN) + P - 1) >> shift;
-                    const int l0 = in_batch * per_tile;              // lane of the tile's first page
-                    // scales of the tile's four parts
-                    const int from = l0 + ((lane & 3) * kPart >> shift);
-                    const int pk = __shfl_sync(0xffffffffu, cur_sk, from), pv = __shfl_sync(0xffffffffu, cur_sv, from);
-                    const unsigned have = __ballot_sync(0xffffffffu, cur_row >= 0) >> l0 & ((1u << pages) - 1u);
-                    const uint32_t bytes = static_cast<uint32_t>(__popc(have)) * P * D;
-                    ok = mbar_wait_warp(&misc->k_empty[x][st], ((kc / C::NK) & 1) ^ 1, misc);
-                    if (!ok) break;
-                    if (lane < 4) {
-                        reinterpret_cast<float*>(&misc->scale_k[x][slot])[lane] = e8m0_value(pk);
-                        reinterpret_cast<float*>(&misc->exp_v[x][slot])[lane] = pv == 255 ? __uint_as_float(0x7fffffffu) : static_cast<float>(pv - 127);
-                    }
-                    if (lane == 0) mbar_expect_tx(kf, bytes);
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(&misc->scale_full[x][slot]);
-                    // the lanes that hold the tile's pages copy them
-                    const int j = lane - l0;
+                    const int pages = (min(kN, key_count - tp * kN) + P - 1) >> shift, j = lane - in_batch * per_tile;
                     const bool copies = j >= 0 && j < pages && cur_row >= 0;
-                    if (copies) tma_load_2d(kt + j * P * D, &maps.page, kf, 0, cur_row);
-                    __syncwarp();
-                    ok = mbar_wait_warp(&misc->c_empty[x][sc], ((kc / C::NC) & 1) ^ 1, misc);
-                    if (!ok) break;
-                    if (lane == 0) mbar_expect_tx(cf, bytes);
-                    if (copies) bulk_load(ct + j * P * D, p.a.page_v + static_cast<int64_t>(cur_row) * D, cf, static_cast<uint32_t>(P) * D);
+                    const uint32_t bytes = static_cast<uint32_t>(__popc(__ballot_sync(0xffffffffu, copies))) * P * D;
+                    if (lane == 0) { mbar_expect_tx(kf, bytes); mbar_expect_tx(cf, bytes); }
+                    if (copies) {
+                        tma_load_2d(kt + j * P * D, &maps.page, kf, 0, cur_row);
+                        bulk_load(ct + j * P * D, p.a.page_v + static_cast<int64_t>(cur_row) * D, cf, static_cast<uint32_t>(P) * D);
+                    }
                     if (in_batch == 1) {
                         const int was = bad;
                         bad = 0;
                         page_scales(nxt_id, head, nxt_row, nxt_sk, nxt_sv);
-                        if (__any_sync(0xffffffffu, bad) && lane == 0 && status) atomicOr(status, HPD_S_BAD_TABLE);
+                        report();
                         bad = was;
+                    }
+                    // The next batch's scales, over those of the batch before this one: the softmax is at most NK + 2 tiles behind, so it has left it.
+                    if (in_batch == per_batch - 1 && tp + 1 < np) {
+                        put_scales(tp / per_batch + 1, nxt_sk, nxt_sv);
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(&misc->batch_full[x]);
                     }
                 }
                 __syncwarp();
+                if (++st == C::NK) { st = 0; k_par ^= 1; }
+                if (++sc == C::NC) { sc = 0; c_par ^= 1; }
+                }
                 if (t == 0) link_pages();
+                if (t == 1) link_scales(w1);
             }
             if (!ok) break;
-            if (nt == 0) link_pages();
-            link_scales(w1);
             w0 = w1; w1 = w2; it0 = it1; it1 = it2;
         }
         }
@@ -414,7 +424,6 @@ attn_paged_kernel(const __grid_constant__ Maps maps, const Params p)
         if (elect_one()) {
             const int x = warp - 1;
             uint32_t qc = 0, tiles = 0;                   // units with tiles so far; tiles of earlier units
-            uint32_t sc = 0, pc = 0;                      // S tiles issued, P tiles consumed
             bool ok = true;
             constexpr uint32_t kHi = D == 128 ? kRows128 : kRows64;
             const uint32_t q_lo = desc_lo(smem_u32(smem + C::OFF_Q + x * C::Q_BYTES));
@@ -423,7 +432,7 @@ attn_paged_kernel(const __grid_constant__ Maps maps, const Params p)
             const uint32_t tmem_s = tmem + x * kColPipe + kColS, tmem_o = tmem + x * kColPipe + kColO;
             const uint32_t idesc_pv = idesc_wide(D);
             for (uint32_t ui = 0; ok; ++ui) {
-                ok = mbar_wait(&misc->desc_full[x], ui & 1, misc);
+                ok = wait_for(&misc->desc_full[x], ui & 1, misc);
                 if (!ok) break;
                 const Unit u = read_unit(misc->desc[x]);
                 mbar_arrive(&misc->desc_empty[x]);
@@ -438,53 +447,47 @@ attn_paged_kernel(const __grid_constant__ Maps maps, const Params p)
                     else if (j == nt - 1) c = last_p;
                     return (c + 15) >> 4;
                 };
-                ok = mbar_wait(&misc->q_full[x], qc & 1, misc);
+                ok = wait_for(&misc->q_full[x], qc & 1, misc);
                 ++qc;
                 auto issue_qk = [&](int j) {
                     const uint32_t kt = tiles + j;
-                    const int ks = kt % C::NK;
+                    const int ks = kt % C::NK, sb = kt & 1;
                     const uint32_t idesc = idesc_codes(cols16(j) << 4);
                     const uint32_t k_lo = k_lo0 + ks * (C::KV_BYTES >> 4);
-                    if (!mbar_wait(&misc->k_full[x][ks], (kt / C::NK) & 1, misc)) return false;
+                    if (!wait_for(&misc->k_full[x][ks], (kt / C::NK) & 1, misc)) return false;
                     tc_fence_after();
                     // k-steps of 32 codes; the low terms of q are a tile (D = 128) or half a row (D = 64) behind the high ones
 #pragma unroll
                     for (int k = 0; k < 2 * D / 32; ++k) {
                         const uint32_t kk = (k % (D / 32)) * 2;
                         const uint32_t qk = k < D / 32 ? kk : (D == 128 ? (kM * 128 >> 4) + kk : 4 + kk);
-                        tc_mma_codes(tmem_s + (sc & 1) * kN, q_lo + qk, kRows128, k_lo + kk, kHi, idesc, k > 0);
+                        tc_mma_codes(tmem_s + sb * kN, q_lo + qk, kRows128, k_lo + kk, kHi, idesc, k > 0);
                     }
+                    tc_commit(&misc->s_full[x][sb]);
                     tc_commit(&misc->k_empty[x][ks]);
-                    tc_commit(&misc->s_full[x][sc & 1]);
                     if (j + 1 >= nt) tc_commit(&misc->q_empty[x]);
-                    ++sc;
                     return true;
                 };
+                // Scores run two tiles ahead: S(j+2) overwrites the tile in which S(j) was computed and P(j) was read, and the tensor core
+                // executes this thread's instructions in the order of issue.  (One tile of scores, handed back as soon as the softmax has them in
+                // registers, and two of P measured 12 % slower.)
                 if (ok) ok = issue_qk(0);
                 if (ok && nt > 1) ok = issue_qk(1);
                 for (int j = 0; j < nt && ok; ++j) {
                     const uint32_t vt = tiles + j;
-                    const int vs = vt % C::NV;
+                    const int vs = vt % C::NV, pb = vt & 1;
                     const uint32_t v_lo = v_lo0 + vs * (C::WIDE_BYTES >> 4);
                     const int nk = cols16(j);
                     const uint32_t acc0 = j >= 1;
-                    const int pb = pc & 1;
-                    ok = mbar_wait(&misc->p_full[x][pb], (pc >> 1) & 1, misc);
+                    if (j == 0 && qc > 1) ok = wait_for(&misc->o_free[x], (qc - 2) & 1, misc);       // the epilogue of the unit before has read O
+                    if (ok) ok = wait_for(&misc->pv_full[x][pb], (vt >> 1) & 1, misc);
                     if (!ok) break;
-                    ok = mbar_wait(&misc->v_full[x][vs], (vt / C::NV) & 1, misc);
-                    if (!ok) break;
-                    if (j == 0 && qc > 1) {               // the epilogue of the unit before has read O
-                        ok = mbar_wait(&misc->o_free[x], (qc - 2) & 1, misc);
-                        if (!ok) break;
-                    }
                     tc_fence_after();
 #pragma unroll
                     for (int k = 0; k < kN / 16; ++k)
                         if (k < nk) tc_mma_ts(tmem_o, tmem_s + pb * kN + k * 8, v_lo + k * 128, idesc_pv, k > 0 ? 1u : acc0);
                     tc_commit(&misc->v_empty[x][vs]);
-                    tc_commit(&misc->p_empty[x][pb]);
                     if (j + 1 >= nt) tc_commit(&misc->o_full[x]);
-                    ++pc;
                     if (j + 2 < nt) ok = issue_qk(j + 2);
                 }
                 tiles += nt;
@@ -495,73 +498,81 @@ attn_paged_kernel(const __grid_constant__ Maps maps, const Params p)
         reg_dealloc<Regs::CONVERT>();
         const int x = (warp - 12) >> 1, half = warp & 1, tid = half * 32 + lane;
         uint8_t* q_tile = smem + C::OFF_Q + x * C::Q_BYTES;
-        const uint8_t* c_ring = smem + C::OFF_C + x * C::NC * C::KV_BYTES;
+        uint8_t* c_ring = smem + C::OFF_C + x * C::NC * C::KV_BYTES;
         uint8_t* v_ring = smem + C::OFF_V + x * C::NV * C::WIDE_BYTES;
         uint32_t tiles = 0, qc = 0;
         bool ok = true;
         for (uint32_t ui = 0; ok; ++ui) {
-            ok = mbar_wait_warp(&misc->desc_full[x], ui & 1, misc);
+            ok = wait_for_warp(&misc->desc_full[x], ui & 1, misc);
             if (!ok) break;
             const UnitDesc& d = misc->desc[x];
             const Unit u = read_unit(d);
             uint32_t cols[kRounds];                       // of this lane's branches: first column and length, for NaN codes
 #pragma unroll
-            for (int r = 0; r < kRounds; ++r) cols[r] = d.cs[lane + 32 * r] | static_cast<uint32_t>(d.len[lane + 32 * r]) << 16;
+            for (int r = 0; r < kRounds; ++r) cols[r] = lane + 32 * r < d.nb_cached ? d.cs[lane + 32 * r] | static_cast<uint32_t>(d.len[lane + 32 * r]) << 16 : 0u;
             __syncwarp();
             if (lane == 0) mbar_arrive(&misc->desc_empty[x]);
             if (u.nt < 0) break;
             if (u.nt == 0) continue;
-            // ---- Q: a row by D/8 lanes, 16 bytes each; a batch of rows is in flight before the tile is free ----
-            constexpr int LANES = D / 8, ROWS = 32 / LANES, BATCH = 6;
+            // ---- Q in place: 16 elements a lane, D/16 lanes a row; a row's 2 D bytes of bf16 become D bytes of high terms and D of low ones ----
+            constexpr int LANES = D / 16, ROWS = 32 / LANES, BATCH = 2;
             const int nrows = u.nb * G, part = lane % LANES;
-            uint4 buf[BATCH];
-            auto row_of = [&](int i) { return (2 * i + half) * ROWS + lane / LANES; };
-            auto fetch = [&](int i0) {
-#pragma unroll
-                for (int i = 0; i < BATCH; ++i) {
-                    const int r = row_of(i0 + i), b = r / G, row = u.row0 + b;
-                    buf[i] = make_uint4(0, 0, 0, 0);
-                    if (r < nrows && row < p.a.a.max_rows)
-                        buf[i] = *reinterpret_cast<const uint4*>(p.a.a.q + (static_cast<int64_t>(row) * p.a.a.g.Hq + u.head * G + (r - b * G)) * D + part * 8);
+            if (half == 0) {
+                ok = wait_for_warp(&misc->q_empty[x], (qc & 1) ^ 1, misc);
+                if (!ok) break;
+                if (elect_one()) {
+                    mbar_expect_tx(&misc->q_raw[x], C::Q_BYTES);
+                    for (int h = 0; h < D / 64; ++h) tma_load_4d(q_tile + h * (kM * 128), &maps.q, &misc->q_raw[x], h * 64, 0, u.head, u.row0);
                 }
-            };
-            fetch(0);
-            ok = mbar_wait_warp(&misc->q_empty[x], (qc & 1) ^ 1, misc);
+                __syncwarp();
+            }
+            ok = wait_for_warp(&misc->q_raw[x], qc & 1, misc);
             if (!ok) break;
             if (lane < 4) misc->nan_branch[x][qc & 1][half][lane] = 0u;
-            for (int i0 = 0; row_of(i0) - lane / LANES < nrows; i0 += BATCH) {
-                if (i0 > 0) fetch(i0);
+            for (int r0 = half * (BATCH * ROWS); r0 < nrows; r0 += 2 * BATCH * ROWS) {
+                // rows of 128 bytes, 16-byte pieces exchanged by the row's number in its group of eight (rows behind the unit's last: whatever is there)
+                auto piece = [&](int r, int c) { return reinterpret_cast<uint4*>(q_tile + (c >> 3) * (kM * 128) + r * 128 + (((c & 7) ^ (r & 7)) << 4)); };
+                uint32_t w[BATCH][8], top[BATCH];         // pairs of elements; largest magnitude of the row (bits)
 #pragma unroll
                 for (int i = 0; i < BATCH; ++i) {
-                    const int r = row_of(i0 + i);
-                    const uint32_t* w = reinterpret_cast<const uint32_t*>(&buf[i]);
-                    int top = 0;
+                    const int r = r0 + i * ROWS + lane / LANES;
+                    const uint4 a = *piece(r, 2 * part), b = *piece(r, 2 * part + 1);
+                    w[i][0] = a.x; w[i][1] = a.y; w[i][2] = a.z; w[i][3] = a.w; w[i][4] = b.x; w[i][5] = b.y; w[i][6] = b.z; w[i][7] = b.w;
+                    uint32_t t2 = 0;
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) top = max(top, max(static_cast<int>(w[k] & 0x7fff), static_cast<int>(w[k] >> 16 & 0x7fff)));
-#pragma unroll
-                    for (int s = 1; s < LANES; s <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, s));
-                    if (r >= nrows) continue;
-                    const int e = min(max(top >> 7, 15), 254);        // exponent byte of the largest; q * 2^(134 - e) is below 256
-                    const float up = __uint_as_float(static_cast<uint32_t>(261 - e) << 23);
-                    uint2 hi, lo;
-#pragma unroll
-                    for (int k = 0; k < 2; ++k) {
-                        const float a = bf16lo(w[2 * k]) * up, b = bf16hi(w[2 * k]) * up, c = bf16lo(w[2 * k + 1]) * up, f = bf16hi(w[2 * k + 1]) * up;
-                        const uint32_t h = e4m3x4(a, b, c, f);
-                        const float2 ab = e4m3x2_value(h & 0xffff), cf = e4m3x2_value(h >> 16);
-                        const uint32_t l = e4m3x4(a - ab.x, b - ab.y, c - cf.x, f - cf.y);
-                        (k ? hi.y : hi.x) = h;
-                        (k ? lo.y : lo.x) = l;
-                    }
-                    // rows of 128 bytes, 16-byte pieces exchanged by the row's number in its group of eight
-                    auto put = [&](uint8_t* tile, int byte, const uint2& v) {
-                        *reinterpret_cast<uint2*>(tile + r * 128 + (((byte >> 4) ^ (r & 7)) << 4) + (byte & 8)) = v;
-                    };
-                    put(q_tile, part * 8, hi);
-                    if (D == 128) put(q_tile + kM * 128, part * 8, lo);
-                    else put(q_tile, 64 + part * 8, lo);
-                    if (part == 0) misc->q_factor[x][r] = top >= 0x7f80 ? __uint_as_float(0x7fffffffu) : __uint_as_float(static_cast<uint32_t>(e - 7) << 23);
+                    for (int k = 0; k < 8; ++k) t2 = __vmaxu2(t2, w[i][k] & 0x7fff7fffu);
+                    top[i] = max(t2 & 0xffffu, t2 >> 16);
                 }
+#pragma unroll
+                for (int s = 1; s < LANES; s <<= 1)
+#pragma unroll
+                    for (int i = 0; i < BATCH; ++i) top[i] = max(top[i], __shfl_xor_sync(0xffffffffu, top[i], s));
+                __syncwarp();                             // every row of the batch has been read
+#pragma unroll
+                for (int i = 0; i < BATCH; ++i) {
+                    const int r = r0 + i * ROWS + lane / LANES;
+                    const uint32_t e = min(max(top[i] >> 7, 15u), 254u);  // exponent byte of the largest; q * 2^(134 - e) is below 256
+                    const float up = __uint_as_float((261u - e) << 23);
+                    uint32_t hi[4], lo[4];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        uint32_t h2[2], l2[2];            // pairs of codes
+#pragma unroll
+                        for (int j = 0; j < 2; ++j) {
+                            const uint32_t e2 = w[i][2 * k + j];
+                            const __half2 v = __floats2half2_rn(bf16lo(e2) * up, bf16hi(e2) * up);        // exact, below 2^-16 to 2^-25
+                            h2[j] = half2_e4m3x2(v);
+                            const uint32_t back = e4m3x2_half2(h2[j]);
+                            l2[j] = half2_e4m3x2(__hsub2(v, *reinterpret_cast<const __half2*>(&back)));
+                        }
+                        hi[k] = h2[0] | h2[1] << 16;
+                        lo[k] = l2[0] | l2[1] << 16;
+                    }
+                    *piece(r, part) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+                    *piece(r, (D == 128 ? 8 : 4) + part) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+                    if (part == 0) misc->q_factor[x][r] = top[i] >= 0x7f80u ? __uint_as_float(0x7fffffffu) : __uint_as_float((e - 7u) << 23);
+                }
+                __syncwarp();
             }
             fence_async_smem();
             __syncwarp();
@@ -572,26 +583,35 @@ attn_paged_kernel(const __grid_constant__ Maps maps, const Params p)
                 const int sc = tiles % C::NC, sv = tiles % C::NV;
                 const bool own = t < ns;
                 const int rows = min(kN, own ? u.stot - t * kN : u.key_count - (t - ns) * kN);       // what lies behind is zero
-                const uint8_t* src = c_ring + sc * C::KV_BYTES;
+                uint8_t* src = c_ring + sc * C::KV_BYTES;
                 uint8_t* dst = v_ring + sv * C::WIDE_BYTES;
-                ok = mbar_wait_warp(&misc->c_full[x][sc], (tiles / C::NC) & 1, misc);
+                ok = wait_for_warp(&misc->c_full[x][sc], (tiles / C::NC) & 1, misc);
                 if (!ok) break;
-                ok = mbar_wait_warp(&misc->v_empty[x][sv], ((tiles / C::NV) & 1) ^ 1, misc);
+                ok = wait_for_warp(&misc->v_empty[x][sv], ((tiles / C::NV) & 1) ^ 1, misc);
                 if (!ok) break;
-                constexpr int PIECES = D / 8;             // of a row: 8 codes each
-#pragma unroll 4
-                for (int i = 0; i < kN * PIECES / 64; ++i) {
-                    const int row = (i * 64 + tid) / PIECES, c = tid % PIECES;
-                    uint2 w = *reinterpret_cast<const uint2*>(src + row * D + c * 8);
-                    if (row >= rows) w = make_uint2(0u, 0u);
-                    if (own) {
-                        // A NaN code must not meet the zero probabilities of other branches' rows: it becomes zero, its branch is noted.  (What
-                        // lies between branches, stale, is no branch's.)
-                        const uint32_t n0 = ((w.x & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u, n1 = ((w.y & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
-                        unsigned hit = __ballot_sync(0xffffffffu, (n0 | n1) != 0);
-                        if (hit) {
-                            w.x &= ~((n0 >> 7) * 0xffu); w.y &= ~((n1 >> 7) * 0xffu);
-                            for (; hit; hit &= hit - 1) {
+                // pieces of 8 codes: 16 bytes of fp16 each, one below another for a thread (rows of 128 bytes, exchanged like q's)
+                constexpr int PIECES = D / 8, STEP = 64 / PIECES, BATCH_V = 8;
+                const int c = tid % PIECES, row = tid / PIECES;
+                uint8_t* from = src + row * D + c * 8;
+                uint8_t* to = dst + (c >> 3) * kVHalf + row * 128 + (((c & 7) ^ row) << 4);
+                const int odd = STEP == 4 ? ((c & 4) ^ (row & 4)) == 0 ? 64 : -64 : 0;                 // where the row's number gains a 4
+                if (own) {
+                    // A NaN code must not meet the zero probabilities of other branches' rows: it becomes zero, its branch is noted.  (What
+                    // lies between branches, stale, is no branch's.)
+                    uint32_t any = 0;
+                    auto nan_of = [](uint32_t v) { return ((v & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; };
+#pragma unroll
+                    for (int i = 0; i < kN / STEP; ++i) {
+                        const uint2 v = *reinterpret_cast<const uint2*>(from + i * STEP * D);
+                        any |= nan_of(v.x) | nan_of(v.y);
+                    }
+                    if (__any_sync(0xffffffffu, any != 0)) {
+#pragma unroll 1
+                        for (int i = 0; i < kN / STEP; ++i) {
+                            uint2* at = reinterpret_cast<uint2*>(from + i * STEP * D);
+                            const uint32_t n0 = nan_of(at->x), n1 = nan_of(at->y);
+                            if (n0 | n1) *at = make_uint2(at->x & ~((n0 >> 7) * 0xffu), at->y & ~((n1 >> 7) * 0xffu));
+                            for (unsigned hit = __ballot_sync(0xffffffffu, (n0 | n1) != 0); hit; hit &= hit - 1) {
                                 const int col = t * kN + (i * 64 + half * 32 + __ffs(hit) - 1) / PIECES;
 #pragma unroll
                                 for (int r = 0; r < kRounds; ++r) {
@@ -602,18 +622,25 @@ attn_paged_kernel(const __grid_constant__ Maps maps, const Params p)
                             }
                         }
                     }
-                    uint4 v;
-                    uint32_t* o = reinterpret_cast<uint32_t*>(&v);
+                }
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2(static_cast<__nv_fp8x2_storage_t>((k < 2 ? w.x : w.y) >> (k & 1) * 16), __NV_E4M3);
-                        o[k] = static_cast<uint32_t>(h.x) | static_cast<uint32_t>(h.y) << 16;
+                for (int i0 = 0; i0 < kN / STEP; i0 += BATCH_V) {
+                    uint2 w[BATCH_V];
+#pragma unroll
+                    for (int i = 0; i < BATCH_V; ++i) w[i] = *reinterpret_cast<const uint2*>(from + (i0 + i) * STEP * D);
+                    if (rows < kN)
+#pragma unroll
+                        for (int i = 0; i < BATCH_V; ++i)
+                            if (row + (i0 + i) * STEP >= rows) w[i] = make_uint2(0u, 0u);
+#pragma unroll
+                    for (int i = 0; i < BATCH_V; ++i) {
+                        const uint4 v = make_uint4(e4m3x2_half2(w[i].x), e4m3x2_half2(w[i].x >> 16), e4m3x2_half2(w[i].y), e4m3x2_half2(w[i].y >> 16));
+                        *reinterpret_cast<uint4*>(to + (i0 + i) * STEP * 128 + ((i0 + i) & 1) * odd) = v;
                     }
-                    *reinterpret_cast<uint4*>(dst + (c >> 3) * kVHalf + row * 128 + (((c & 7) ^ (row & 7)) << 4)) = v;
                 }
                 fence_async_smem();
                 __syncwarp();
-                if (lane == 0) { mbar_arrive(&misc->v_full[x][sv]); mbar_arrive(&misc->c_empty[x][sc]); }
+                if (lane == 0) { mbar_arrive(&misc->pv_full[x][tiles & 1]); mbar_arrive(&misc->c_empty[x][sc]); }
             }
             ++qc;
         }
@@ -626,18 +653,19 @@ attn_paged_kernel(const __grid_constant__ Maps maps, const Params p)
         const uint32_t lane_base = static_cast<uint32_t>(quad * 32) << 16;
         const uint32_t tmem_s0 = tmem + lane_base + x * kColPipe + kColS;
         const uint32_t tmem_o = tmem + lane_base + x * kColPipe + kColO;
-        uint8_t* stg = smem + C::OFF_STAGE + (x * 4 + quad) * 2048;      // this warp's output staging
-        const int b_row = row / G;                       // branch of this row inside the unit
-        const uint32_t g_magic = 0xFFFFFFFFu / static_cast<uint32_t>(G) + 1u;   // floor(r / G) = umulhi(r, g_magic) for r < 2^16, G > 1
-        uint32_t pw = 0, qc = 0;                         // tiles done (S read, P written), units with tiles
+        uint8_t* stg = smem + C::OFF_STAGE + (x * 4 + quad) * 1024;      // this warp's output staging
+        const int b_row = row >> g_shift;                // branch of this row inside the unit
+        const int shift = 31 - __clz(p.a.page_size);
+        uint32_t pw = 0, qc = 0, batches = 0;            // tiles done (S read, P written), units with tiles, batches of pages beyond the first
         bool ok = true;
         for (uint32_t unit_idx = 0; ok; ++unit_idx) {
-            ok = mbar_wait_warp(&misc->desc_full[x], unit_idx & 1, misc);
+            ok = wait_for_warp(&misc->desc_full[x], unit_idx & 1, misc);
             if (!ok) break;
             const UnitDesc& d = misc->desc[x];
             const Unit u = read_unit(d);
-            const int my_cs = d.cs[b_row], my_len = d.len[b_row];
-            const float my_k = e8m0_value(d.ks[b_row]), my_e = d.vs[b_row] == 255 ? __uint_as_float(0x7fffffffu) : static_cast<float>(d.vs[b_row] - 127);
+            const bool cached = b_row < d.nb_cached;
+            const int my_cs = cached ? d.cs[b_row] : 0, my_len = cached ? d.len[b_row] : 0;
+            const float my_k = e8m0_value(cached ? d.ks[b_row] : 127), my_e = !cached ? 0.f : d.vs[b_row] == 255 ? __uint_as_float(0x7fffffffu) : static_cast<float>(d.vs[b_row] - 127);
             __syncwarp();
             if (lane == 0) mbar_arrive(&misc->desc_empty[x]);
             if (u.nt < 0) break;
@@ -647,7 +675,7 @@ attn_paged_kernel(const __grid_constant__ Maps maps, const Params p)
             const bool warp_active = quad * 32 < nrows;
             float q_factor = 0.f;
             if (nt > 0) {
-                ok = mbar_wait_warp(&misc->q_full[x], qc & 1, misc);
+                ok = wait_for_warp(&misc->q_full[x], qc & 1, misc);
                 if (!ok) break;
                 q_factor = misc->q_factor[x][row] * p.scale_log2;
                 __syncwarp();
@@ -655,148 +683,186 @@ attn_paged_kernel(const __grid_constant__ Maps maps, const Params p)
             }
             float R = -INFINITY, M = -INFINITY, l = 0.f;
             const int j_full = ns + u.key_count / kN;    // tiles [ns, j_full): every row sees them whole
-            for (int j = 0; j < nt && ok; ++j) {
-                int lo = 0, hi = kN;
-                bool vis = warp_active, whole = true;
-                if (warp_active && (j < ns || j >= j_full)) {
-                    if (j >= ns) {
-                        hi = u.key_count - (j - ns) * kN;
-                    } else {
-                        const int base = j * kN;
-                        lo = max(0, my_cs - base);
-                        hi = min(kN, my_cs + my_len - base);
-                        if (hi < lo) hi = lo;
+            // References of the row from a tile's largest score and largest product (log2): taken as they are by a row that has seen nothing so far,
+            // moved when one has grown by more than the slack (probabilities and sums are at most 2^8 larger until then).  False: gave up.
+            auto refer = [&](float top_s, float top_r) {
+                const bool fresh = R == -INFINITY;       // O row is still exactly zero
+                if (fresh) { R = top_r; M = top_s; }
+                const bool grow = top_r > R + kRescaleSlack || top_s > M + kRescaleSlack;
+                if (__any_sync(0xffffffffu, grow)) {
+                    // O must be rescaled: wait until the previous P V product has landed in TMEM.  (In a unit's first tile all rows are fresh.)
+                    if (!wait_for_warp(&misc->v_empty[x][(pw - 1) % C::NV], ((pw - 1) / C::NV) & 1, misc)) return false;
+                    tc_fence_after();
+                    const float r_new = grow ? fmaxf(R, top_r) : R, m_new = grow ? fmaxf(M, top_s) : M;
+                    const float f = grow ? ex2(R - r_new) : 1.f;
+                    if (grow) l *= ex2(M - m_new);
+#pragma unroll 1
+                    for (int c0 = 0; c0 < D; c0 += 32) {
+                        uint32_t ov[32];
+                        tmem_ld32(tmem_o + c0, ov);
+                        tmem_ld_wait();
+#pragma unroll
+                        for (int c = 0; c < 32; ++c) ov[c] = __float_as_uint(__uint_as_float(ov[c]) * f);
+                        tmem_st32(tmem_o + c0, ov);
                     }
-                    vis = __any_sync(0xffffffffu, row_valid && hi > lo);
-                    whole = __all_sync(0xffffffffu, lo == 0 && hi == kN);
+                    tmem_st_wait();
+                    R = r_new;
+                    M = m_new;
                 }
+                return true;
+            };
+            auto factor = [&](float k) {                 // of raw scores; not zero: masked scores are -inf (NaN stays)
+                k *= q_factor;
+                return k < 1.17549435e-38f ? 1.17549435e-38f : k;
+            };
+            auto largest16 = [](const uint32_t* s) {
+                float a = fmaxf(__uint_as_float(s[0]), __uint_as_float(s[1])), b = fmaxf(__uint_as_float(s[2]), __uint_as_float(s[3]));
+#pragma unroll
+                for (int k = 4; k < kPart; k += 4) {
+                    a = fmax3(a, __uint_as_float(s[k]), __uint_as_float(s[k + 1]));
+                    b = fmax3(b, __uint_as_float(s[k + 2]), __uint_as_float(s[k + 3]));
+                }
+                return fmaxf(a, b);
+            };
+            // V exponent less the reference, raised for a part whose products stay below 2^-60 of it: ms is the part's largest score
+            auto exponent = [&](float ev, float ms) {
+                const float ref = R == -INFINITY ? 0.f : R;
+                return fminf(fmaxf(ev, ref - kFaint - ms), 400.f) - ref + (ev - ev);       // NaN stays
+            };
+            // The probabilities of 16 columns of one scale as fp16 pairs, and their share of the sum.
+            auto probabilities = [&](const uint32_t* s, float k, float e, uint32_t* pk) {
+                const uint64_t k2 = pair(k, k), e2 = pair(e + kUp, e + kUp);
+                uint64_t sum = pair(0.f, 0.f);
+#pragma unroll
+                for (int i = 0; i < kPart / 2; ++i) {
+                    const uint64_t y = fma2(pair(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1])), k2, e2);
+                    float y0, y1;
+                    unpair(y, y0, y1);
+                    const float e0 = ex2(y0), e1 = ex2(y1);
+                    sum = add2(sum, pair(e0, e1));
+                    const __half2 two = __floats2half2_rn(e0, e1);
+                    pk[i] = *reinterpret_cast<const uint32_t*>(&two);
+                }
+                float a0, a1;
+                unpair(sum, a0, a1);
+                l = fmaf(a0 + a1, ex2(-e - kUp - (M == -INFINITY ? 0.f : M)), l);
+            };
+            for (int j = 0; j < nt && ok; ++j) {
                 const int pb = pw & 1;                   // the tile's S / P buffer
                 const uint32_t tmem_s = tmem_s0 + pb * kN;
-                float ksc[4], ev[4];                     // of the tile's parts: factor of the scores, V exponent
-                ok = mbar_wait_warp(&misc->scale_full[x][pw % kScaleSlots], (pw / kScaleSlots) & 1, misc);
-                if (!ok) break;
-                if (j >= ns) {
-                    const float4 a = misc->scale_k[x][pw % kScaleSlots], b = misc->exp_v[x][pw % kScaleSlots];
-                    ksc[0] = a.x; ksc[1] = a.y; ksc[2] = a.z; ksc[3] = a.w;
-                    ev[0] = b.x; ev[1] = b.y; ev[2] = b.z; ev[3] = b.w;
-                } else {
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) { ksc[c] = my_k; ev[c] = my_e; }
+                // K scale and V exponent of the tile's c-th part
+                const int first_page = (j - ns) << (6 - shift);
+                auto scale_of = [&](int c) { return j < ns ? make_float2(my_k, my_e) : misc->page_scale[x][unit_idx & 1][(first_page + (c * kPart >> shift)) & 63]; };
+                if (j > ns && (first_page & 31) == 0) {  // the next 32 pages
+                    ok = wait_for_warp(&misc->batch_full[x], batches & 1, misc);
+                    if (!ok) break;
+                    ++batches;
                 }
-#pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    ksc[c] *= q_factor;
-                    if (ksc[c] < 1.17549435e-38f) ksc[c] = 1.17549435e-38f;          // not zero: masked scores are -inf (NaN stays)
-                }
-                ok = mbar_wait_warp(&misc->s_full[x][pb], (pw >> 1) & 1, misc);
+                ok = wait_for_warp(&misc->s_full[x][pb], (pw >> 1) & 1, misc);
                 if (!ok) break;
                 tc_fence_after();
-                if (vis) {
+                if (!warp_active) {                      // no rows: nobody reads its probabilities' products
+                } else if (j >= ns && j < j_full) {
                     uint32_t sv[kN];
                     tmem_ld32(tmem_s, sv); tmem_ld32(tmem_s + 32, sv + 32);
-                    tmem_ld_wait();
-                    if (!whole) {
-                        const unsigned span = static_cast<unsigned>(hi - lo);
+                    float k[4], ev[4], ms[4];            // of the tile's parts: factor of the scores, V exponent, largest score
 #pragma unroll
-                        for (int c = 0; c < kN; ++c)
-                            if (static_cast<unsigned>(c - lo) >= span) sv[c] = 0xff800000u;   // -inf
-                    }
-                    float top_s = -INFINITY, top_r = -INFINITY, ms[4];
+                    for (int c = 0; c < 4; ++c) { const float2 sc = scale_of(c); k[c] = factor(sc.x); ev[c] = sc.y; }
+                    tmem_ld_wait();
+                    float top_s = -INFINITY, top_r = -INFINITY, low_r = INFINITY;
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
-                        const uint32_t* s = sv + c * kPart;
-                        float a = fmaxf(__uint_as_float(s[0]), __uint_as_float(s[1])), b = fmaxf(__uint_as_float(s[2]), __uint_as_float(s[3]));
-#pragma unroll
-                        for (int k = 4; k < kPart; k += 4) {
-                            a = fmax3(a, __uint_as_float(s[k]), __uint_as_float(s[k + 1]));
-                            b = fmax3(b, __uint_as_float(s[k + 2]), __uint_as_float(s[k + 3]));
-                        }
-                        ms[c] = fmaxf(a, b) * ksc[c];
+                        ms[c] = largest16(sv + c * kPart) * k[c];
                         top_s = fmaxf(top_s, ms[c]);
                         top_r = fmaxf(top_r, ms[c] + ev[c]);
+                        low_r = fminf(low_r, ms[c] + ev[c]);
                     }
-                    const float m_new = fmaxf(M, top_s);
-                    if (m_new > M && M != -INFINITY) l *= ex2(M - m_new);
-                    M = m_new;
-                    {
-                        const bool fresh = R == -INFINITY;       // nothing visible so far: O row is still exactly zero
-                        if (fresh) R = top_r;
-                        const bool grow = !fresh && top_r > R + kRescaleSlack;
-                        if (__any_sync(0xffffffffu, grow)) {
-                            // O must be rescaled: wait until the previous P V product has landed in TMEM.  (In a unit's first tile all rows are fresh.)
-                            ok = mbar_wait_warp(&misc->p_empty[x][(pw - 1) & 1], ((pw - 1) >> 1) & 1, misc);
-                            if (ok) {
-                                tc_fence_after();
-                                const float r_new = grow ? top_r : R;
-                                const float f = grow ? ex2(R - r_new) : 1.f;
-#pragma unroll 1
-                                for (int c0 = 0; c0 < D; c0 += 32) {
-                                    uint32_t ov[32];
-                                    tmem_ld32(tmem_o + c0, ov);
-                                    tmem_ld_wait();
-#pragma unroll
-                                    for (int c = 0; c < 32; ++c) ov[c] = __float_as_uint(__uint_as_float(ov[c]) * f);
-                                    tmem_st32(tmem_o + c0, ov);
-                                }
-                                tmem_st_wait();
-                                R = r_new;
-                            }
-                        }
-                    }
+                    ok = refer(top_s, top_r);
                     if (!ok) break;
-                    // Probabilities go to tensor memory as fp16 pairs, over the first half of the row's own scores.
-                    const float ref = R == -INFINITY ? 0.f : R, sum_ref = (M == -INFINITY ? 0.f : M) + kUp;
+                    if (__any_sync(0xffffffffu, !(low_r >= R - kFaint))) {
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {        // 32 keys = 16 columns of pairs per store
+                        for (int c = 0; c < 4; ++c) ev[c] = exponent(ev[c], ms[c]);
+                    } else {
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) ev[c] -= R;
+                    }
+                    // to tensor memory, over the first half of the row's own scores: 32 keys = 16 columns of pairs per store
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
                         uint32_t pk[16];
 #pragma unroll
-                        for (int c2 = 0; c2 < 2; ++c2) {
-                            const int c = 2 * h + c2;
-                            const float e = fminf(fmaxf(ev[c], ref - kFaint - ms[c]), 400.f) - ref + (ev[c] - ev[c]);       // NaN stays
-                            const uint64_t k2 = pair(ksc[c], ksc[c]), e2 = pair(e + kUp, e + kUp);
-                            uint64_t sum = pair(0.f, 0.f);
-#pragma unroll
-                            for (int k = 0; k < kPart / 2; ++k) {
-                                const uint64_t y = fma2(pair(__uint_as_float(sv[c * kPart + 2 * k]), __uint_as_float(sv[c * kPart + 2 * k + 1])), k2, e2);
-                                float y0, y1;
-                                unpair(y, y0, y1);
-                                const float e0 = ex2(y0), e1 = ex2(y1);
-                                sum = add2(sum, pair(e0, e1));
-                                const __half2 two = __floats2half2_rn(e0, e1);
-                                pk[c2 * 8 + k] = *reinterpret_cast<const uint32_t*>(&two);
-                            }
-                            float a0, a1;
-                            unpair(sum, a0, a1);
-                            l = fmaf(a0 + a1, ex2(-e - sum_ref), l);
-                        }
+                        for (int c2 = 0; c2 < 2; ++c2)
+                            probabilities(sv + (2 * h + c2) * kPart, k[2 * h + c2], ev[2 * h + c2], pk + c2 * 8);
                         tmem_st16(tmem_s + h * 16, pk);
                     }
                     tmem_st_wait();
-                } else if (warp_active) {                // nothing visible for any row of the warp: zero probabilities
-                    uint32_t pk[16];
+                } else {
+                    // A tile of branches' tokens, or a document's last: columns [lo, hi) of this row, parts [c_lo, c_hi) of the warp's rows; the other parts'
+                    // probabilities are zero.
+                    int lo = 0, hi = u.key_count - (j - ns) * kN;
+                    if (j < ns) {
+                        lo = max(0, my_cs - j * kN);
+                        hi = min(kN, my_cs + my_len - j * kN);
+                    }
+                    const bool sees = row_valid && hi > lo;
+                    const int c_lo = __reduce_min_sync(0xffffffffu, sees ? lo : kN) / kPart;
+                    const int c_hi = (__reduce_max_sync(0xffffffffu, sees ? hi : 0) + kPart - 1) / kPart;
+                    // Part by part, twice: the largest score first.  (P of a part lies over scores that have been used.)
+                    auto part = [&](int c, uint32_t (&sv)[kPart]) {
+                        tmem_ld16(tmem_s + c * kPart, sv);
+                        const int from = lo - c * kPart;
+                        const unsigned span = sees ? static_cast<unsigned>(hi - lo) : 0u;
+                        tmem_ld_wait();
 #pragma unroll
-                    for (int c = 0; c < 16; ++c) pk[c] = 0u;
-                    tmem_st16(tmem_s, pk);
-                    tmem_st16(tmem_s + 16, pk);
+                        for (int i = 0; i < kPart; ++i)
+                            if (static_cast<unsigned>(i - from) >= span) sv[i] = 0xff800000u;       // -inf
+                    };
+                    float top_s = -INFINITY, top_r = -INFINITY;
+#pragma unroll 1
+                    for (int c = c_lo; c < c_hi; ++c) {
+                        uint32_t sv[kPart];
+                        part(c, sv);
+                        const float2 sc = scale_of(c);
+                        const float ms = largest16(sv) * factor(sc.x);
+                        top_s = fmaxf(top_s, ms);
+                        top_r = fmaxf(top_r, ms + sc.y);
+                    }
+                    ok = c_hi <= c_lo || refer(top_s, top_r);
+                    if (!ok) break;
+#pragma unroll 1
+                    for (int c = 0; c < kN / kPart; ++c) {
+                        uint32_t pk[8];
+                        if (c >= c_lo && c < c_hi) {
+                            uint32_t sv[kPart];
+                            part(c, sv);
+                            const float2 sc = scale_of(c);
+                            const float k = factor(sc.x);
+                            probabilities(sv, k, exponent(sc.y, largest16(sv) * k), pk);
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) pk[i] = 0u;
+                        }
+                        tmem_st8(tmem_s + c * 8, pk);
+                    }
                     tmem_st_wait();
                 }
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(&misc->p_full[x][pb]);
+                if (lane == 0) mbar_arrive(&misc->pv_full[x][pb]);
                 ++pw;
             }
             if (!ok) break;
 
             // ------------------------------------ epilogue ------------------------------------
             if (nt > 0) {                                // the unit's last P V product has landed (and the P tile is free)
-                ok = mbar_wait_warp(&misc->o_full[x], qc & 1, misc);
+                ok = wait_for_warp(&misc->o_full[x], qc & 1, misc);
                 if (!ok) break;
                 const volatile uint32_t* nan = &misc->nan_branch[x][qc & 1][0][0];
                 if (ns > 0 && (nan[b_row >> 5] | nan[4 + (b_row >> 5)]) >> (b_row & 31) & 1) l = __uint_as_float(0x7fffffffu);
                 ++qc;
             }
             tc_fence_after();
-            const int g_row = row - b_row * G;
+            const int g_row = row & (G - 1);
             const int grow_row = u.row0 + b_row;
             const int hq = u.head * G + g_row;
             const bool store = row_valid && grow_row < p.a.a.max_rows;
@@ -829,29 +895,27 @@ attn_paged_kernel(const __grid_constant__ Maps maps, const Params p)
                 for (int c0 = 0; c0 < D; c0 += 32) {
                     float acc[32];
                     read_o(c0, acc);
-                    // transpose through this warp's 2 KB of shared memory: a row's 32 columns go out as one 64-byte
-                    // piece, 8 rows per store instruction
+                    // transpose through this warp's 1 KB of shared memory, 16 columns at a time: a row's go out as one 32-byte
+                    // piece, 16 rows per store instruction
 #pragma unroll
-                    for (int c = 0; c < 32; c += 8) {
-                        uint4 pk;
-                        pk.x = pack_bf16(acc[c + 0], acc[c + 1]);
-                        pk.y = pack_bf16(acc[c + 2], acc[c + 3]);
-                        pk.z = pack_bf16(acc[c + 4], acc[c + 5]);
-                        pk.w = pack_bf16(acc[c + 6], acc[c + 7]);
-                        *reinterpret_cast<uint4*>(stg + lane * 64 + ((((c >> 3) ^ (lane >> 1)) & 3) << 4)) = pk;
-                    }
-                    __syncwarp();
+                    for (int c1 = 0; c1 < 32; c1 += 16) {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int rl = 8 * i + (lane >> 2), ch = lane & 3;       // row inside the warp's 32, 16-byte piece
-                        const uint4 pk = *reinterpret_cast<const uint4*>(stg + rl * 64 + (((ch ^ (rl >> 1)) & 3) << 4));
-                        const int trow = quad * 32 + rl;
-                        const int tb = G == 1 ? trow : static_cast<int>(__umulhi(static_cast<uint32_t>(trow), g_magic)), tg = trow - tb * G;
-                        const int grow = u.row0 + tb;
-                        if (trow < nrows && grow < p.a.a.max_rows)
-                            *reinterpret_cast<uint4*>(p.a.a.o + (static_cast<int64_t>(grow) * p.a.a.g.Hq + u.head * G + tg) * D + c0 + ch * 8) = pk;
+                        for (int c = 0; c < 2; ++c) {
+                            const float* a = acc + c1 + 8 * c;
+                            *reinterpret_cast<uint4*>(stg + lane * 32 + (((c ^ (lane >> 2)) & 1) << 4)) =
+                                make_uint4(pack_bf16(a[0], a[1]), pack_bf16(a[2], a[3]), pack_bf16(a[4], a[5]), pack_bf16(a[6], a[7]));
+                        }
+                        __syncwarp();
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            const int rl = 16 * i + (lane >> 1), ch = lane & 1;  // row inside the warp's 32, 16-byte piece
+                            const uint4 pk = *reinterpret_cast<const uint4*>(stg + rl * 32 + (((ch ^ (rl >> 2)) & 1) << 4));
+                            const int trow = quad * 32 + rl, tb = trow >> g_shift, grow = u.row0 + tb;
+                            if (trow < nrows && grow < p.a.a.max_rows)
+                                *reinterpret_cast<uint4*>(p.a.a.o + (static_cast<int64_t>(grow) * p.a.a.g.Hq + u.head * G + (trow & (G - 1))) * D + c0 + c1 + ch * 8) = pk;
+                        }
+                        __syncwarp();
                     }
-                    __syncwarp();
                 }
             } else {
 #pragma unroll 1
@@ -923,7 +987,7 @@ int launch_d(const PagedArgs& a)
     const void* pages = page_rows > 0 ? static_cast<const void*>(a.page_k) : a.a.q;
     const void* branches = branch_rows > 0 ? static_cast<const void*>(a.branch_k) : a.a.q;
     Maps maps;
-    bool ok = make_codes_map(&maps.page, pages, D, std::max(page_rows, 1ll), a.page_size);
+    bool ok = make_q_map(&maps.q, a.a.q, D, g.Hq / g.Hkv, g.Hkv, a.a.max_rows) && make_codes_map(&maps.page, pages, D, std::max(page_rows, 1ll), a.page_size);
     for (int i = 0; i < 16 && ok; ++i) ok = make_codes_map(&maps.branch[i], branches, D, std::max(branch_rows, 1ll), i + 1);
     if (!ok) {
         set_last_cuda_error(cudaErrorInvalidValue);

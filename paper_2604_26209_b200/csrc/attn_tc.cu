@@ -1023,22 +1023,6 @@ bool make_kv_map(CUtensorMap* m, const void* base, int D, int Hkv, long long tok
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// q [rows, Hkv, G, D] bf16: boxes of 128/G rows x 1 kv head x G x 64 elements -> tile row = branch*G + g
-bool make_q_map(CUtensorMap* m, const void* base, int D, int G, int Hkv, long long rows)
-{
-    auto fn = tensor_map_encoder();
-    if (!fn) return false;
-    cuuint64_t dims[4] = {static_cast<cuuint64_t>(D), static_cast<cuuint64_t>(G), static_cast<cuuint64_t>(Hkv),
-                          static_cast<cuuint64_t>(rows > 0 ? rows : 1)};
-    cuuint64_t strides[3] = {static_cast<cuuint64_t>(D) * 2, static_cast<cuuint64_t>(G) * D * 2,
-                             static_cast<cuuint64_t>(Hkv) * G * D * 2};
-    cuuint32_t box[4] = {64, static_cast<cuuint32_t>(G), 1, static_cast<cuuint32_t>(kM / G)};
-    cuuint32_t es[4] = {1, 1, 1, 1};
-    return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims, strides, box, es,
-              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
 TcParams make_params(const AttnArgs& a)
 {
     TcParams p{};

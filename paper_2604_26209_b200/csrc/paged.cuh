@@ -1,6 +1,7 @@
 // The 8-bit page format: e4m3 codes and one power-of-two scale (an e8m0 byte) per page, kv head, and key or value.
 #pragma once
 
+#include <cuda_fp16.h>
 #include <cuda_fp8.h>
 #include <stdint.h>
 
@@ -36,10 +37,23 @@ __device__ __forceinline__ uint32_t e4m3x4(float a, float b, float c, float d)
     const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(c, d), __NV_SATFINITE, __NV_E4M3);
     return lo | hi << 16;
 }
+// two codes (the low half of a word) as fp16, which holds every code exactly, and back (as above)
+__device__ __forceinline__ uint32_t e4m3x2_half2(uint32_t two)
+{
+    uint32_t h;
+    asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, a;\n\t}" : "=r"(h) : "r"(two));
+    return h;
+}
+__device__ __forceinline__ uint32_t half2_e4m3x2(__half2 h)
+{
+    uint16_t two;
+    asm("cvt.rn.satfinite.e4m3x2.f16x2 %0, %1;" : "=h"(two) : "r"(*reinterpret_cast<const uint32_t*>(&h)));
+    return two;
+}
 __device__ __forceinline__ float2 e4m3x2_value(uint32_t two)
 {
-    const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2(static_cast<__nv_fp8x2_storage_t>(two), __NV_E4M3);
-    return __half22float2(__half2(h));
+    const uint32_t h = e4m3x2_half2(two);
+    return __half22float2(*reinterpret_cast<const __half2*>(&h));
 }
 // four codes times a power of two
 __device__ __forceinline__ uint32_t e4m3x4_times(uint32_t w, float f)
