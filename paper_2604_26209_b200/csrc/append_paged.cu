@@ -59,11 +59,16 @@ __device__ __forceinline__ void rotate_chunk(Chunk& c, const float* cs, const fl
 }
 __device__ __forceinline__ int chunk_top(const Chunk& c)
 {
-    int top = 0;
-    const uint32_t* l = reinterpret_cast<const uint32_t*>(&c.lo);
-    const uint32_t* h = reinterpret_cast<const uint32_t*>(&c.hi);
+    const uint32_t w[8] = {c.lo.x, c.lo.y, c.lo.z, c.lo.w, c.hi.x, c.hi.y, c.hi.z, c.hi.w};
+    uint32_t two = 0;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) { top = max_finite(top, l[w]); top = max_finite(top, h[w]); }
+    for (int i = 0; i < 8; ++i) two = __vmaxu2(two, w[i] & 0x7fff7fffu);
+    int top = static_cast<int>(max(two & 0xffffu, two >> 16));
+    if (top >= 0x7f80) {                             // infinities or NaN among them, which do not count: element by element
+        top = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) top = max_finite(top, w[i]);
+    }
     return top;
 }
 __device__ __forceinline__ uint2 codes8(const uint4& x, float inv)
@@ -85,6 +90,21 @@ __device__ __forceinline__ void rescale16(uint8_t* p, int was, int now)
     *reinterpret_cast<uint4*>(p) = w;
 }
 
+// the same for units u, u + 32, u + 64 and u + 96 of `units`, their loads together
+__device__ __forceinline__ void rescale16x4(uint8_t* p, int u, int units, int was, int now)
+{
+    const float f = now - was < 127 ? __uint_as_float(static_cast<uint32_t>(127 - (now - was)) << 23) : 0.f;
+    uint4* q = reinterpret_cast<uint4*>(p);
+    uint4 w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (u + 32 * i < units) w[i] = q[u + 32 * i];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (u + 32 * i < units)
+            q[u + 32 * i] = make_uint4(e4m3x4_times(w[i].x, f), e4m3x4_times(w[i].y, f), e4m3x4_times(w[i].z, f), e4m3x4_times(w[i].w, f));
+}
+
 // Page of token `index` of table row `entry`: -1 and a status bit where there is none.
 __device__ __forceinline__ int page_of(const PageArgs& p, int entry, int64_t index, bool report)
 {
@@ -104,10 +124,10 @@ __device__ __forceinline__ int page_of(const PageArgs& p, int entry, int64_t ind
 // ------------------------------------------------------------------------------------------------
 // One token per sequence: the decode step.  Row r is sequence r's token.
 // ------------------------------------------------------------------------------------------------
-constexpr int kStepThreads = 128, kStepRows = 2, kStepBatch = 3;
+constexpr int kStepThreads = 128, kStepRows = 2, kStepBatch = 3, kStepResident = 8;
 
 template <int D>
-__global__ void __launch_bounds__(kStepThreads)
+__global__ void __launch_bounds__(kStepThreads, kStepResident)
 append_step_kernel(int Hq /* 0: no queries */, int Hkv, const InvFreq inv_freq, const PageArgs p)
 {
     constexpr int HALF = D / 2, CH = D / 16;         // chunk pairs of a head: CH consecutive lanes
@@ -121,9 +141,10 @@ append_step_kernel(int Hq /* 0: no queries */, int Hkv, const InvFreq inv_freq, 
     const int items = (2 * Hkv + Hq) * CH;           // of one row: its keys, its values, its queries
     const int total = nr * items;
     auto source = [&](int it, int& row, int& head, int& ch) -> const __nv_bfloat16* {
-        row = it / items;
-        const int local = it - row * items;
-        head = local / CH; ch = local - head * CH;
+        static_assert(kStepRows == 2, "row by comparison");
+        row = it >= items;
+        const int local = row ? it - items : it;
+        head = local / CH; ch = local % CH;
         const int64_t r = r0 + row;
         if (head < Hkv) return p.k_new + (r * Hkv + head) * D;
         if (head < 2 * Hkv) return p.v_new + (r * Hkv + head - Hkv) * D;
@@ -154,161 +175,213 @@ append_step_kernel(int Hq /* 0: no queries */, int Hkv, const InvFreq inv_freq, 
     __syncthreads();
     for (int base = 0; base < total; base += kStepBatch * parts * kStepThreads) {
         if (base > 0) fetch(base);
+        int was[kStepBatch];                         // scales of before, asked for together; 0: the page is new (or it is a query)
 #pragma unroll
         for (int k = 0; k < kStepBatch; ++k) {
             const int it = base + threadIdx.x + (k * parts + part) * kStepThreads;
-            if (it >= total) continue;
-            int row, head, ch;
-            (void)source(it, row, head, ch);
-            const bool is_v = head >= Hkv && head < 2 * Hkv;
-            if (p.pos_id && !is_v) rotate_chunk(c[k], cs[row] + ch * 8, sn[row] + ch * 8);
-            if (head >= 2 * Hkv) {
-                store_chunk<D>(p.q_rot + (static_cast<int64_t>(r0 + row) * Hq + head - 2 * Hkv) * D, ch, c[k]);
-                continue;
+            was[k] = 0;
+            if (it < total) {
+                int row, head, ch;
+                (void)source(it, row, head, ch);
+                if (head < 2 * Hkv && s_page[row] >= 0 && s_slot[row] > 0)
+                    was[k] = head < Hkv ? p.scale_k[static_cast<int64_t>(s_page[row]) * Hkv + head] : p.scale_v[static_cast<int64_t>(s_page[row]) * Hkv + head - Hkv];
             }
-            // a head's CH lanes, a group inside the warp, agree on its scale
-            const unsigned group = (CH == 32 ? 0xffffffffu : ((1u << CH) - 1u)) << (threadIdx.x & 31 & ~(CH - 1));
-            int top = chunk_top(c[k]);
+        }
 #pragma unroll
-            for (int s = 1; s < CH; s <<= 1) top = max(top, __shfl_xor_sync(group, top, s));
-            const int page = s_page[row], slot = s_slot[row];
-            if (page < 0) continue;
-            const int64_t ph = static_cast<int64_t>(page) * Hkv + (is_v ? head - Hkv : head);
-            uint8_t* scale = (is_v ? p.scale_v : p.scale_k) + ph;
+        for (int k = 0; k < kStepBatch; ++k) {
+            const int it = base + threadIdx.x + (k * parts + part) * kStepThreads;
+            const bool have = it < total;
+            int row = 0, head = 2 * Hkv, ch = 0;
+            if (have) (void)source(it, row, head, ch);
+            const bool is_v = head >= Hkv && head < 2 * Hkv;
+            if (have && p.pos_id && !is_v) rotate_chunk(c[k], cs[row] + ch * 8, sn[row] + ch * 8);
+            if (have && head >= 2 * Hkv) store_chunk<D>(p.q_rot + (static_cast<int64_t>(r0 + row) * Hq + head - 2 * Hkv) * D, ch, c[k]);
+            // a head's CH lanes agree on its scale
+            const bool kept = have && head < 2 * Hkv && s_page[row] >= 0;
+            int top = kept ? chunk_top(c[k]) : 0;
+#pragma unroll
+            for (int s = 1; s < CH; s <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, s));
+            const int slot = s_slot[row], now = max(e8m0_needed(top), was[k]);
+            const long long ph = kept ? static_cast<long long>(s_page[row]) * Hkv + (is_v ? head - Hkv : head) : 0;
             uint8_t* codes = (is_v ? p.page_v : p.page_k) + ph * p.page_size * D;
-            int now = e8m0_needed(top);
-            if (slot > 0) {
-                const int was = *scale;
-                if (now > was) {
-                    // 16 codes a lane: token by token, D/16 = CH lanes each
-                    for (int t = 0; t < slot; ++t) rescale16(codes + static_cast<int64_t>(t) * D + ch * 16, was, now);
-                } else {
-                    now = was;
-                }
-                __syncwarp(group);                   // every lane of the group has the old scale
+            // Codes held under a smaller scale, by the whole warp, four loads of 16 in flight: by the head's lanes alone, token by token, a step of
+            // 6144 rows of which a few per cent of the heads need it took 38.5 us.
+            for (unsigned m = __ballot_sync(0xffffffffu, kept && ch == 0 && slot > 0 && now > was[k]); m; m &= m - 1) {
+                const int from = __ffs(m) - 1;
+                uint8_t* at = reinterpret_cast<uint8_t*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(codes), from));
+                const int units = __shfl_sync(0xffffffffu, slot, from) * CH, was_m = __shfl_sync(0xffffffffu, was[k], from), now_m = __shfl_sync(0xffffffffu, now, from);
+                for (int u = threadIdx.x & 31; u < units; u += 128) rescale16x4(at, u, units, was_m, now_m);
             }
-            store_codes<D>(codes + static_cast<int64_t>(slot) * D, ch, c[k], e8m0_inverse(now));
-            if (ch == 0) *scale = static_cast<uint8_t>(now);
+            if (kept) {
+                store_codes<D>(codes + static_cast<int64_t>(slot) * D, ch, c[k], e8m0_inverse(now));
+                if (ch == 0) (is_v ? p.scale_v : p.scale_k)[ph] = static_cast<uint8_t>(now);
+            }
         }
     }
 }
 
 // ------------------------------------------------------------------------------------------------
-// Any number of tokens per sequence: prompts and chunks.  The rows of a sequence that go into one page are a segment; a CTA takes
-// the segments that begin in its window of page_size rows, for every gridDim.y-th kv head and that head's queries.
+// Any number of tokens per sequence: prompts and chunks.  The rows of a sequence that go into one page are a segment.  A CTA has the
+// segments that begin in its window of 64 rows and takes them in groups of up to 64 rows, for every gridDim.y-th kv head and those heads' queries:
+// the angles of a group's rows are computed once.
 // ------------------------------------------------------------------------------------------------
-constexpr int kTokThreads = 256, kTokRows = 64, kTokQueries = 4;
+constexpr int kTokThreads = 256, kTokRows = 64, kTokQueries = 2;
+template <int D> constexpr int kTokResident = D == 128 ? 3 : 4;       // CTAs of an SM
 
 template <int D>
-__global__ void __launch_bounds__(kTokThreads)
+__global__ void __launch_bounds__(kTokThreads, kTokResident<D>)
 append_tokens_kernel(int Hq /* 0: no queries */, int Hkv, const InvFreq inv_freq, const PageArgs p)
 {
     constexpr int HALF = D / 2, CH = D / 16;
     constexpr int B = kTokRows * CH / kTokThreads;   // chunk pairs of one head's keys (or values) a thread holds
     __shared__ float cs[kTokRows][HALF], sn[kTokRows][HALF];
-    __shared__ int s_top[2][kTokThreads / 32];
+    __shared__ int s_seg[kTokRows], s_slot[kTokRows];                        // per row: its segment in the group, its place in the page
+    __shared__ int g_page[kTokRows], g_held[kTokRows];                       // per segment: page (-1: none), tokens that it held
+    __shared__ int g_top[2][2][kTokRows], g_was[2][2][kTokRows];             // per parity of the head, K / V and segment: largest magnitude, scale of before
+    __shared__ uint32_t s_starts[2];
+    __shared__ int s_end;
     const int n = min(*p.n_rows, p.max_rows);
-    const int P = p.page_size, G = Hq / Hkv;
-    const int64_t lo = static_cast<int64_t>(blockIdx.x) * P;
-    const int end = static_cast<int>(min(lo + P, static_cast<int64_t>(n)));
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    for (int r = static_cast<int>(min(lo, static_cast<int64_t>(n))), stop; r < end; r = stop) {
-        // ---- the segment that begins at row r, or the rest of one that another window has ----
-        const int seq = p.row_seq[r];
-        int page = -1, slot = 0;
-        stop = r + 1;
-        if (seq < 0 || seq >= p.n_seqs || r < p.seq_row_start[seq] || r >= p.seq_row_start[seq + 1]) {
-            if (threadIdx.x == 0 && blockIdx.y == 0 && p.dev_status) atomicOr(p.dev_status, HPD_S_BAD_TABLE);
-        } else {
-            const int first = p.seq_row_start[seq], past = min(p.seq_row_start[seq + 1], n);
-            const int64_t index = static_cast<int64_t>(p.seq_len[seq]) + (r - first);
-            slot = static_cast<int>(index < 0 ? 0 : index % P);
-            stop = min(past, r + P - slot);
-            if (r != first && slot != 0) continue;
-            page = page_of(p, p.seq_id ? p.seq_id[seq] : seq, index, threadIdx.x == 0 && blockIdx.y == 0);
+    const int P = p.page_size, G = Hq / Hkv, q_shift = 31 - __clz(max(G, 1) * CH);
+    const int64_t lo = static_cast<int64_t>(blockIdx.x) * kTokRows;
+    const int end = static_cast<int>(min(lo + kTokRows, static_cast<int64_t>(n)));
+    const int t0 = threadIdx.x;
+    for (int r = static_cast<int>(min(lo, static_cast<int64_t>(n))); r < end;) {
+        // ---- the group's rows: where they go, where segments begin ----
+        __syncthreads();                             // the tables of the group before have been used
+        if (t0 == 0) s_end = r;
+        __syncthreads();
+        int entry = -1, slot = 0, stop = 0;
+        int64_t index = 0;
+        bool start = false;
+        if (t0 < kTokRows) {
+            const int row = r + t0;
+            if (row < n) {
+                const int seq = p.row_seq[row];
+                const int first = seq >= 0 && seq < p.n_seqs ? p.seq_row_start[seq] : 0, past = seq >= 0 && seq < p.n_seqs ? p.seq_row_start[seq + 1] : 0;
+                if (row < first || row >= past) {    // of no sequence: a segment of its own without a page
+                    start = true; stop = row + 1;
+                } else {
+                    index = static_cast<int64_t>(p.seq_len[seq]) + (row - first);
+                    slot = static_cast<int>(index < 0 ? 0 : index % P);
+                    start = row == first || slot == 0;
+                    stop = min(min(past, n), row + P - slot);
+                    entry = p.seq_id ? p.seq_id[seq] : seq;
+                    if (index < 0 || entry < 0) entry = -1;
+                }
+            }
+            const unsigned starts = __ballot_sync(0xffffffffu, start);
+            if ((t0 & 31) == 0) s_starts[t0 >> 5] = starts;
         }
-        const int rows = stop - r;
-        if (p.pos_id) {
-            __syncthreads();                         // the angles of the segment before have been used
-            for (int i = threadIdx.x; i < rows * HALF; i += kTokThreads) {
+        __syncthreads();
+        const uint64_t starts = s_starts[0] | static_cast<uint64_t>(s_starts[1]) << 32;
+        if (!(starts & 1)) {                         // the window begins inside a segment, which another one has
+            r = starts ? r + __ffsll(static_cast<long long>(starts)) - 1 : r + kTokRows;
+            continue;
+        }
+        if (t0 < kTokRows) {
+            const int seg = __popcll(starts & (~0ull >> (63 - t0))) - 1;
+            s_seg[t0] = seg; s_slot[t0] = slot;
+            if (starts >> t0 & 1) {
+                int page = -1;
+                if (entry >= 0) page = page_of(p, entry, index, blockIdx.y == 0);
+                else if (blockIdx.y == 0 && p.dev_status) atomicOr(p.dev_status, HPD_S_BAD_TABLE);
+                g_page[seg] = page; g_held[seg] = page < 0 ? 0 : slot;
+                if (r + t0 < end && stop - r <= kTokRows) atomicMax(&s_end, stop);       // later ones are another window's
+            }
+        }
+        __syncthreads();
+        const int rows = s_end - r;                  // whole segments only: the first one at least
+        const int segs = __popcll(starts & (~0ull >> (64 - rows)));
+        if (p.pos_id)
+            for (int i = t0; i < rows * HALF; i += kTokThreads) {
                 const int t = i / HALF, a = i % HALF;
                 rotary_angle(p.pos_id[r + t], inv_freq.f[a], cs[t][a], sn[t][a]);
             }
-            __syncthreads();
-        }
-        for (int h = blockIdx.y; h < Hkv; h += gridDim.y) {
-            if (page >= 0) {
-                Chunk k[B], v[B];
-                bool mine[B];                        // rows that the two tables agree on
+        // ---- head by head: while the keys and values are on their way, the head's queries ----
+        for (int h = blockIdx.y, par = 0; h < Hkv; h += gridDim.y, par ^= 1) {
+            Chunk k[B], v[B];
 #pragma unroll
-                for (int b = 0; b < B; ++b) {
-                    const int it = threadIdx.x + b * kTokThreads, t = it / CH;
-                    mine[b] = t < rows && p.row_seq[r + t] == seq;
-                    if (t < rows && !mine[b] && h == 0 && p.dev_status) atomicOr(p.dev_status, HPD_S_BAD_TABLE);
-                    if (t < rows) {
-                        const int64_t at = (static_cast<int64_t>(r + t) * Hkv + h) * D;
-                        k[b] = load_chunk<D>(p.k_new + at, it % CH);
-                        v[b] = load_chunk<D>(p.v_new + at, it % CH);
-                    }
+            for (int b = 0; b < B; ++b) {
+                const int it = t0 + b * kTokThreads, t = it / CH;
+                if (t < rows) {
+                    const int64_t at = (static_cast<int64_t>(r + t) * Hkv + h) * D;
+                    k[b] = load_chunk<D>(p.k_new + at, it % CH);
+                    v[b] = load_chunk<D>(p.v_new + at, it % CH);
                 }
-                const int64_t ph = static_cast<int64_t>(page) * Hkv + h;
-                const int was_k = slot > 0 ? p.scale_k[ph] : 0, was_v = slot > 0 ? p.scale_v[ph] : 0;
-                int top_k = 0, top_v = 0;
-#pragma unroll
-                for (int b = 0; b < B; ++b) {
-                    const int it = threadIdx.x + b * kTokThreads, t = it / CH;
-                    if (mine[b]) {
-                        if (p.pos_id) rotate_chunk(k[b], cs[t] + it % CH * 8, sn[t] + it % CH * 8);
-                        top_k = max(top_k, chunk_top(k[b]));
-                        top_v = max(top_v, chunk_top(v[b]));
-                    }
-                }
-                top_k = __reduce_max_sync(0xffffffffu, top_k);
-                top_v = __reduce_max_sync(0xffffffffu, top_v);
-                if (lane == 0) { s_top[0][warp] = top_k; s_top[1][warp] = top_v; }
-                __syncthreads();                     // ... and everybody has the scales of before
-#pragma unroll
-                for (int w = 0; w < kTokThreads / 32; ++w) { top_k = max(top_k, s_top[0][w]); top_v = max(top_v, s_top[1][w]); }
-                const int now_k = max(e8m0_needed(top_k), was_k), now_v = max(e8m0_needed(top_v), was_v);
-                uint8_t* codes_k = p.page_k + ph * P * D;
-                uint8_t* codes_v = p.page_v + ph * P * D;
-                if (now_k > was_k)
-                    for (int i = threadIdx.x; i < slot * (D / 16); i += kTokThreads) rescale16(codes_k + i * 16, was_k, now_k);
-                if (now_v > was_v)
-                    for (int i = threadIdx.x; i < slot * (D / 16); i += kTokThreads) rescale16(codes_v + i * 16, was_v, now_v);
-                const float inv_k = e8m0_inverse(now_k), inv_v = e8m0_inverse(now_v);
-#pragma unroll
-                for (int b = 0; b < B; ++b) {
-                    const int it = threadIdx.x + b * kTokThreads, t = it / CH;
-                    if (mine[b]) {
-                        store_codes<D>(codes_k + (slot + t) * D, it % CH, k[b], inv_k);
-                        store_codes<D>(codes_v + (slot + t) * D, it % CH, v[b], inv_v);
-                    }
-                }
-                if (threadIdx.x == 0) { p.scale_k[ph] = static_cast<uint8_t>(now_k); p.scale_v[ph] = static_cast<uint8_t>(now_v); }
-                __syncthreads();                     // s_top is free again
             }
-            // ---- the queries of this kv head ----
-            const int per_row = G * CH, total = rows * per_row;
-            for (int base = 0; base < total; base += kTokQueries * kTokThreads) {
+            if (t0 < 2 * kTokRows && t0 % kTokRows < segs) {
+                const int seg = t0 % kTokRows, is_v = t0 / kTokRows;
+                g_top[par][is_v][seg] = 0;
+                g_was[par][is_v][seg] = g_held[seg] > 0 ? (is_v ? p.scale_v : p.scale_k)[static_cast<int64_t>(g_page[seg]) * Hkv + h] : 0;
+            }
+            __syncthreads();
+            const int per_row = G * CH, total = rows * per_row;      // a power of two: G is 1, 2, 4 or 8
+            auto at = [&](int it) { return (static_cast<int64_t>(r + (it >> q_shift)) * Hq + h * G + (it & (per_row - 1)) / CH) * D; };
+            for (int base = t0; base < total; base += kTokQueries * kTokThreads) {
                 Chunk c[kTokQueries];
-                auto at = [&](int it) { return (static_cast<int64_t>(r + it / per_row) * Hq + h * G + it % per_row / CH) * D; };
 #pragma unroll
                 for (int b = 0; b < kTokQueries; ++b) {
-                    const int it = base + threadIdx.x + b * kTokThreads;
+                    const int it = base + b * kTokThreads;
                     if (it < total) c[b] = load_chunk<D>(p.q + at(it), it % CH);
                 }
 #pragma unroll
                 for (int b = 0; b < kTokQueries; ++b) {
-                    const int it = base + threadIdx.x + b * kTokThreads;
+                    const int it = base + b * kTokThreads;
                     if (it < total) {
-                        const int t = it / per_row;
-                        rotate_chunk(c[b], cs[t] + it % CH * 8, sn[t] + it % CH * 8);
+                        rotate_chunk(c[b], cs[it >> q_shift] + it % CH * 8, sn[it >> q_shift] + it % CH * 8);
                         store_chunk<D>(p.q_rot + at(it), it % CH, c[b]);
                     }
                 }
             }
+#pragma unroll
+            for (int b = 0; b < B; ++b) {
+                const int it = t0 + b * kTokThreads, t = it / CH, ch = it % CH;
+                int top_k = 0, top_v = 0;
+                if (t < rows) {
+                    if (p.pos_id) rotate_chunk(k[b], cs[t] + ch * 8, sn[t] + ch * 8);
+                    top_k = chunk_top(k[b]);
+                    top_v = chunk_top(v[b]);
+                }
+                // a token's CH lanes, then the segment's tokens
+#pragma unroll
+                for (int s = 1; s < CH; s <<= 1) {
+                    top_k = max(top_k, __shfl_xor_sync(0xffffffffu, top_k, s));
+                    top_v = max(top_v, __shfl_xor_sync(0xffffffffu, top_v, s));
+                }
+                if (t < rows && ch == 0) { atomicMax(&g_top[par][0][s_seg[t]], top_k); atomicMax(&g_top[par][1][s_seg[t]], top_v); }
+            }
+            __syncthreads();
+            auto now_of = [&](int is_v, int seg) { return max(e8m0_needed(g_top[par][is_v][seg]), g_was[par][is_v][seg]); };
+#pragma unroll
+            for (int b = 0; b < B; ++b) {
+                const int it = t0 + b * kTokThreads, t = it / CH, ch = it % CH;
+                if (t < rows) {
+                    const int seg = s_seg[t];
+                    if (g_page[seg] >= 0) {
+                        const int64_t at = ((static_cast<int64_t>(g_page[seg]) * Hkv + h) * P + s_slot[t]) * D;
+                        store_codes<D>(p.page_k + at, ch, k[b], e8m0_inverse(now_of(0, seg)));
+                        store_codes<D>(p.page_v + at, ch, v[b], e8m0_inverse(now_of(1, seg)));
+                    }
+                }
+            }
+            // pages that held tokens under a smaller scale: few, at most the first of each sequence
+            for (int seg = 0; seg < segs; ++seg) {
+                const int held = g_held[seg];
+                if (held == 0) continue;
+                const int64_t ph = static_cast<int64_t>(g_page[seg]) * Hkv + h;
+                for (int is_v = 0; is_v < 2; ++is_v) {
+                    const int was = g_was[par][is_v][seg], now = now_of(is_v, seg);
+                    uint8_t* codes = (is_v ? p.page_v : p.page_k) + ph * P * D;
+                    if (now > was)
+                        for (int i = t0; i < held * (D / 16); i += kTokThreads) rescale16(codes + i * 16, was, now);
+                }
+            }
+            if (t0 < 2 * kTokRows && t0 % kTokRows < segs) {
+                const int seg = t0 % kTokRows, is_v = t0 / kTokRows;
+                if (g_page[seg] >= 0) (is_v ? p.scale_v : p.scale_k)[static_cast<int64_t>(g_page[seg]) * Hkv + h] = static_cast<uint8_t>(now_of(is_v, seg));
+            }
         }
+        r = s_end;
     }
 }
 
@@ -330,8 +403,9 @@ int launch_append_paged(const hpd_geom& g, const AppendPagedArgs& a)
         if (wide) append_step_kernel<128><<<grid, kStepThreads, 0, a.stream>>>(Hq, g.Hkv, f, p);
         else append_step_kernel<64><<<grid, kStepThreads, 0, a.stream>>>(Hq, g.Hkv, f, p);
     } else {
-        const unsigned windows = (static_cast<unsigned>(a.max_rows) + a.page_size - 1) / a.page_size;
-        const dim3 grid(windows, static_cast<unsigned>(g.Hkv));
+        // few rows: the heads of a window go to several CTAs, up to two waves of three an SM
+        const unsigned windows = (static_cast<unsigned>(a.max_rows) + kTokRows - 1) / kTokRows;
+        const dim3 grid(windows, std::min<unsigned>(g.Hkv, std::max(1u, 3u * sm_count() / windows)));
         if (wide) append_tokens_kernel<128><<<grid, kTokThreads, 0, a.stream>>>(Hq, g.Hkv, f, p);
         else append_tokens_kernel<64><<<grid, kTokThreads, 0, a.stream>>>(Hq, g.Hkv, f, p);
     }

@@ -74,7 +74,7 @@ static_assert(Cfg<128>::SMEM <= 232448, "shared memory budget");
 struct Maps {
     CUtensorMap q;                         // bf16: boxes of 128/G rows x G heads x 64 elements
     CUtensorMap page;                      // K codes of the documents: boxes of one page
-    CUtensorMap branch[16];                // K codes of the branches: boxes of 1 .. 16 tokens
+    CUtensorMap branch[16];                // K codes of the branches: boxes of 1 .. 16 tokens (of a page at most)
 };
 
 struct Params {
@@ -986,9 +986,9 @@ int launch_d(const PagedArgs& a)
     const long long page_rows = static_cast<long long>(a.n_pages) * g.Hkv * a.page_size, branch_rows = static_cast<long long>(a.n_branch_pages) * g.Hkv * g.suffix_cap;
     const void* pages = page_rows > 0 ? static_cast<const void*>(a.page_k) : a.a.q;
     const void* branches = branch_rows > 0 ? static_cast<const void*>(a.branch_k) : a.a.q;
-    Maps maps;
+    Maps maps{};
     bool ok = make_q_map(&maps.q, a.a.q, D, g.Hq / g.Hkv, g.Hkv, a.a.max_rows) && make_codes_map(&maps.page, pages, D, std::max(page_rows, 1ll), a.page_size);
-    for (int i = 0; i < 16 && ok; ++i) ok = make_codes_map(&maps.branch[i], branches, D, std::max(branch_rows, 1ll), i + 1);
+    for (int i = 0; i < std::min(16, g.suffix_cap) && ok; ++i) ok = make_codes_map(&maps.branch[i], branches, D, std::max(branch_rows, 1ll), i + 1);
     if (!ok) {
         set_last_cuda_error(cudaErrorInvalidValue);
         return HPD_E_CUDA;
