@@ -184,6 +184,82 @@ class SharedBlockBatch:
         self.attn_two_pass() if two_pass else self.attn()
 
 
+class PagedBatch:
+    """One layer's decode state over paged caches in 8 bits: the documents in pages of ``page_size`` tokens, every branch in a page of suffix_cap tokens of
+    a second pool.  A step is ``build_meta`` -> ``append`` (rotation and quantisation of the step's tokens) -> ``attn``; the caches are filled from a
+    batch's bf16 tensors by the same append, the documents in one call, the branches' earlier tokens step by step."""
+
+    def __init__(self, s: Structure, t: Dict[str, np.ndarray], page_size: int = 64, device="cuda"):
+        db = DeviceBatch(s, t, device, posorder=False)
+        self.db, self.s, self.g = db, s, s.geom
+        i32 = lambda a: torch.from_numpy(np.ascontiguousarray(a, dtype=np.int32)).to(device)
+        length = np.asarray(s.doc_prefix_len, np.int64)
+        need = -(-length // page_size)
+        per_doc = max(1, int(need.max(initial=0)))
+        self.docs = B.PagedCache.alloc(self.g, s.n_docs, per_doc, page_size, int(need.sum()), device)
+        first = np.concatenate([[0], np.cumsum(need)])[:-1]
+        table = np.where(np.arange(per_doc)[None, :] < need[:, None], first[:, None] + np.arange(per_doc)[None, :], -1)
+        if s.n_docs:
+            self.docs.table.copy_(i32(table))
+        self.branches = B.PagedCache.alloc(self.g, s.n_slots, 1, self.g.suffix_cap, device=device)
+        self.q_rot = torch.zeros_like(db.q)
+        self.o, self.lse = db.o, db.lse
+        self._status = db.meta.dev_status
+        self._load(i32, length)
+        for name in ("prefix_k", "prefix_v", "suffix_k", "suffix_v"):                     # the bf16 caches are not needed any more
+            setattr(db, name, None)
+
+    def _load(self, i32, length):
+        """The batch's cached keys and values (already rotated) into the pages."""
+        s, g, db = self.s, self.g, self.db
+        if s.total_prefix:
+            start = np.concatenate([[0], np.cumsum(length)])
+            B.hpd_append_paged(g, s.n_docs, s.total_prefix, i32([s.total_prefix]), i32(np.repeat(np.arange(s.n_docs), length)), i32(start), None,
+                               i32(np.zeros(s.n_docs)), self.docs, None, None, None, db.prefix_k, db.prefix_v, self._status)
+        for depth in range(int(s.slot_depth.max()) if s.n_slots else 0):
+            slots = np.flatnonzero(s.slot_depth > depth)
+            rows = torch.from_numpy(slots * g.suffix_cap + depth).to(db.q.device)
+            k, v = (x.view(-1, g.Hkv, g.D)[rows].contiguous() for x in (db.suffix_k, db.suffix_v))
+            B.hpd_append_paged(g, len(slots), len(slots), i32([len(slots)]), None, None, i32(slots), i32(np.full(len(slots), depth)), self.branches, None,
+                               None, None, k, v, self._status)
+
+    def build_meta(self):
+        self.db.build_meta()
+
+    def set_step_inputs(self, q_rows: np.ndarray, k_rows: np.ndarray, v_rows: np.ndarray):
+        self.db.set_step_inputs(q_rows, k_rows, v_rows)
+
+    def append(self):
+        db, m, n = self.db, self.db.meta, self.s.n_slots
+        B.hpd_append_paged(self.g, n, n, m.n_active, None, None, m.active_slot, m.suffix_len, self.branches, m.pos_id, db.q, self.q_rot, db.k_new,
+                           db.v_new, m.dev_status)
+
+    def attn(self, suffix_includes_new=True, lse=True):
+        db, s = self.db, self.s
+        B.hpd_attn_decode_paged(self.g, s.n_docs, s.n_slots, s.n_slots, self.q_rot, self.docs, self.branches, db.doc_prefix_len, db.meta,
+                                suffix_includes_new, self.o, self.lse if lse else None)
+
+    def step(self, with_meta=True):
+        if with_meta:
+            self.build_meta()
+        self.append()
+        self.attn()
+
+    def capture_step(self, with_meta=True):
+        """The step's launches in a CUDA graph (call step() at least once before)."""
+        g = torch.cuda.CUDAGraph()
+        torch.cuda.synchronize()
+        with torch.cuda.graph(g):
+            self.step(with_meta=with_meta)
+        return g
+
+    def tables(self) -> Dict[str, np.ndarray]:
+        return self.db.tables()
+
+    def status(self) -> int:
+        return self.db.status()
+
+
 class DupBatch:
     """Duplicated-prefix layout for ``std_attn_decode``: every active row gets a private physical copy
     [its document's prefix ; its cached branch tokens (new token included)].  Built with torch gathers
