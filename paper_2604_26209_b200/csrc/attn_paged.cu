@@ -23,6 +23,7 @@
 // All waits are bounded: a wait that gives up raises HPD_S_TIMEOUT in the status word and the CTA drains and exits.
 #include <algorithm>
 #include <atomic>
+#include <type_traits>
 
 #include <cuda_fp16.h>
 
@@ -65,7 +66,7 @@ template <int D> struct Cfg {
     static constexpr int OFF_C = OFF_K + 2 * NK * KV_BYTES;
     static constexpr int OFF_V = OFF_C + 2 * NC * KV_BYTES;
     static constexpr int OFF_MISC = OFF_V + 2 * NV * WIDE_BYTES;
-    static constexpr int SMEM = OFF_MISC + 6144;
+    static constexpr int SMEM = OFF_MISC + 8192;
     static_assert(OFF_V % 1024 == 0 && OFF_K % 1024 == 0, "swizzled tiles");
     static_assert(NK + 2 < 8, "a batch of pages has at least eight tiles");
 };
@@ -104,16 +105,17 @@ struct Misc {
     unsigned long long q_raw[2], q_full[2], q_empty[2];          // q as it is has come; its two terms are there; the tile is free
     unsigned long long k_full[2][kMaxStages], k_empty[2][kMaxStages], c_full[2][kMaxStages], c_empty[2][kMaxStages], v_empty[2][kMaxStages];
     unsigned long long s_full[2][2], pv_full[2][2], o_full[2], o_free[2];        // pv: the probabilities and the widened V tile
-    unsigned long long desc_full[2], desc_empty[2], batch_full[2];
+    unsigned long long desc_full[2], desc_empty[2], batch_full[2], meet[2];
     uint32_t tmem_base;
     int abort_flag;
     int pad[2];
     float2 page_scale[2][2][64];           // pipeline, unit's parity: K scale and V exponent of the document's pages, two batches of 32
     float q_factor[2][kM];                 // what the scaled rows of q have to be multiplied by
+    float2 way_ml[2][kM];                  // reference and sum of every row of the tile, where they are two ways' (see ways_of)
     uint32_t nan_branch[2][2][2][4];       // pipeline, unit's parity, conversion warp: branches with a NaN among their values
     UnitDesc desc[2];
 };
-static_assert(sizeof(Misc) <= 6144, "misc block");
+static_assert(sizeof(Misc) <= 8192, "misc block");
 
 // Bounded wait: false once two to four seconds (2^32 cycles and more) have passed or another thread of the CTA has given up.  Short on purpose: it stands
 // at some forty places, and the kernel's code competes for the instruction cache (138 KB of it cost 8 % against 80).
@@ -142,12 +144,19 @@ __device__ __forceinline__ uint32_t desc_lo_mnmajor(uint32_t saddr) { return (sa
 __device__ __forceinline__ uint32_t idesc_codes(int N) { return (1u << 4) | (static_cast<uint32_t>(N >> 3) << 17) | (static_cast<uint32_t>(kM >> 4) << 24); }
 __device__ __forceinline__ uint32_t idesc_wide(int N) { return idesc_codes(N) | (1u << 16); }
 
+// Units of up to 64 rows and at least kTwoTiles tiles have their rows twice in the tile: rows 0-63 take the first half of every tile's keys, rows 64-127 the
+// second, each with references and sums of their own; the epilogue adds them up, 3 k cycles more.  A tile's softmax is then half as long, and that is
+// what most of a tile's time is (192 documents of 1024 to 4096 tokens, 12 branches of 4 heads: 337 -> 285 us).
+// In a kernel of its own, for steps whose documents have 64 rows or fewer on average: the code for both in one cost the others 4 %.
+constexpr int kTwoTiles = 8;
+template <bool TWO> __device__ __forceinline__ int ways_of(int nrows, int nt) { return TWO && nrows <= kM / 2 && nt >= kTwoTiles ? 2 : 1; }
+
 struct Unit { int nt, np, stot, head, key_count, part_base, row_begin, nb, row0; };
 __device__ __forceinline__ Unit read_unit(const UnitDesc& d) {
     return {d.nt, d.np, d.stot, d.head, d.key_count, d.part_base, d.row_begin, d.nb, d.row0};
 }
 
-template <int D>
+template <int D, bool TWO>
 __global__ void __launch_bounds__(kThreads, 1)
 attn_paged_kernel(const __grid_constant__ Maps maps, const Params p)
 {
@@ -172,7 +181,7 @@ attn_paged_kernel(const __grid_constant__ Maps maps, const Params p)
                 mbar_init(&misc->c_full[i][k], 1); mbar_init(&misc->c_empty[i][k], 2);
                 mbar_init(&misc->v_empty[i][k], 1);
             }
-            mbar_init(&misc->batch_full[i], 1);
+            mbar_init(&misc->batch_full[i], 1); mbar_init(&misc->meet[i], 4);
         }
         misc->abort_flag = 0;
         fence_mbar_init();
@@ -516,7 +525,7 @@ attn_paged_kernel(const __grid_constant__ Maps maps, const Params p)
             if (u.nt == 0) continue;
             // ---- Q in place: 16 elements a lane, D/16 lanes a row; a row's 2 D bytes of bf16 become D bytes of high terms and D of low ones ----
             constexpr int LANES = D / 16, ROWS = 32 / LANES, BATCH = 2;
-            const int nrows = u.nb * G, part = lane % LANES;
+            const int nrows = u.nb * G, ways = ways_of<TWO>(nrows, u.nt), part = lane % LANES;
             if (half == 0) {
                 ok = wait_for_warp(&misc->q_empty[x], (qc & 1) ^ 1, misc);
                 if (!ok) break;
@@ -568,9 +577,12 @@ attn_paged_kernel(const __grid_constant__ Maps maps, const Params p)
                         hi[k] = h2[0] | h2[1] << 16;
                         lo[k] = l2[0] | l2[1] << 16;
                     }
-                    *piece(r, part) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-                    *piece(r, (D == 128 ? 8 : 4) + part) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
-                    if (part == 0) misc->q_factor[x][r] = top[i] >= 0x7f80u ? __uint_as_float(0x7fffffffu) : __uint_as_float((e - 7u) << 23);
+                    const float factor = top[i] >= 0x7f80u ? __uint_as_float(0x7fffffffu) : __uint_as_float((e - 7u) << 23);
+                    for (int w = 0; w < ways; ++w) {
+                        *piece(r + w * (kM / 2), part) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+                        *piece(r + w * (kM / 2), (D == 128 ? 8 : 4) + part) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+                        if (part == 0) misc->q_factor[x][r + w * (kM / 2)] = factor;
+                    }
                 }
                 __syncwarp();
             }
@@ -654,15 +666,17 @@ attn_paged_kernel(const __grid_constant__ Maps maps, const Params p)
         const uint32_t tmem_s0 = tmem + lane_base + x * kColPipe + kColS;
         const uint32_t tmem_o = tmem + lane_base + x * kColPipe + kColO;
         uint8_t* stg = smem + C::OFF_STAGE + (x * 4 + quad) * 1024;      // this warp's output staging
-        const int b_row = row >> g_shift;                // branch of this row inside the unit
         const int shift = 31 - __clz(p.a.page_size);
-        uint32_t pw = 0, qc = 0, batches = 0;            // tiles done (S read, P written), units with tiles, batches of pages beyond the first
+        uint32_t pw = 0, qc = 0, batches = 0, meets = 0; // tiles done (S read, P written), units with tiles, batches of pages beyond the first, meetings
         bool ok = true;
         for (uint32_t unit_idx = 0; ok; ++unit_idx) {
             ok = wait_for_warp(&misc->desc_full[x], unit_idx & 1, misc);
             if (!ok) break;
             const UnitDesc& d = misc->desc[x];
             const Unit u = read_unit(d);
+            const int nrows = u.nb * G, ways = ways_of<TWO>(nrows, u.nt), way = ways == 2 ? quad >> 1 : 0;
+            const int u_row = row - way * (kM / 2);      // row of the unit
+            const int b_row = u_row >> g_shift;          // its branch inside the unit
             const bool cached = b_row < d.nb_cached;
             const int my_cs = cached ? d.cs[b_row] : 0, my_len = cached ? d.len[b_row] : 0;
             const float my_k = e8m0_value(cached ? d.ks[b_row] : 127), my_e = !cached ? 0.f : d.vs[b_row] == 255 ? __uint_as_float(0x7fffffffu) : static_cast<float>(d.vs[b_row] - 127);
@@ -670,14 +684,14 @@ attn_paged_kernel(const __grid_constant__ Maps maps, const Params p)
             if (lane == 0) mbar_arrive(&misc->desc_empty[x]);
             if (u.nt < 0) break;
             const int nt = u.nt, ns = nt - u.np;
-            const int nrows = u.nb * G;
-            const bool row_valid = row < nrows;
-            const bool warp_active = quad * 32 < nrows;
+            const bool row_valid = u_row < nrows;
+            const bool warp_active = quad * 32 - way * (kM / 2) < nrows;
             float q_factor = 0.f;
             if (nt > 0) {
                 ok = wait_for_warp(&misc->q_full[x], qc & 1, misc);
                 if (!ok) break;
-                q_factor = misc->q_factor[x][row] * p.scale_log2;
+                // rows behind the unit's last hold anything: their scores are made zero, or they would have the warp rescale O in every tile
+                q_factor = row_valid ? misc->q_factor[x][row] * p.scale_log2 : 0.f;
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&misc->q_empty[x]);
             }
@@ -747,6 +761,50 @@ attn_paged_kernel(const __grid_constant__ Maps maps, const Params p)
                 unpair(sum, a0, a1);
                 l = fmaf(a0 + a1, ex2(-e - kUp - (M == -INFINITY ? 0.f : M)), l);
             };
+            // A document's tile that every row sees whole: PARTS parts of it from `first` on (four, or the half of this way's rows; the other half's
+            // probabilities are zero).
+            auto whole = [&](auto parts, int first, uint32_t tmem_s, auto& scale_of) {
+                constexpr int PARTS = decltype(parts)::value;
+                uint32_t sv[PARTS * kPart];
+#pragma unroll
+                for (int h = 0; h < PARTS / 2; ++h) tmem_ld32(tmem_s + (first + 2 * h) * kPart, sv + h * 32);
+                float k[PARTS], ev[PARTS], ms[PARTS];    // of the parts: factor of the scores, V exponent, largest score
+#pragma unroll
+                for (int c = 0; c < PARTS; ++c) { const float2 sc = scale_of(first + c); k[c] = factor(sc.x); ev[c] = sc.y; }
+                tmem_ld_wait();
+                float top_s = -INFINITY, top_r = -INFINITY, low_r = INFINITY;
+#pragma unroll
+                for (int c = 0; c < PARTS; ++c) {
+                    ms[c] = largest16(sv + c * kPart) * k[c];
+                    top_s = fmaxf(top_s, ms[c]);
+                    top_r = fmaxf(top_r, ms[c] + ev[c]);
+                    low_r = fminf(low_r, ms[c] + ev[c]);
+                }
+                if (!refer(top_s, top_r)) return false;
+                if (__any_sync(0xffffffffu, !(low_r >= R - kFaint))) {
+#pragma unroll
+                    for (int c = 0; c < PARTS; ++c) ev[c] = exponent(ev[c], ms[c]);
+                } else {
+#pragma unroll
+                    for (int c = 0; c < PARTS; ++c) ev[c] -= R;
+                }
+                // to tensor memory, over the first half of the row's own scores: 32 keys = 16 columns of pairs per store
+#pragma unroll
+                for (int h = 0; h < PARTS / 2; ++h) {
+                    uint32_t pk[16];
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) probabilities(sv + (2 * h + c) * kPart, k[2 * h + c], ev[2 * h + c], pk + c * 8);
+                    tmem_st16(tmem_s + (first + 2 * h) * (kPart / 2), pk);
+                }
+                if (PARTS < 4) {
+                    uint32_t pk[16];
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) pk[i] = 0u;
+                    tmem_st16(tmem_s + (first ^ 2) * (kPart / 2), pk);
+                }
+                tmem_st_wait();
+                return true;
+            };
             for (int j = 0; j < nt && ok; ++j) {
                 const int pb = pw & 1;                   // the tile's S / P buffer
                 const uint32_t tmem_s = tmem_s0 + pb * kN;
@@ -763,39 +821,9 @@ attn_paged_kernel(const __grid_constant__ Maps maps, const Params p)
                 tc_fence_after();
                 if (!warp_active) {                      // no rows: nobody reads its probabilities' products
                 } else if (j >= ns && j < j_full) {
-                    uint32_t sv[kN];
-                    tmem_ld32(tmem_s, sv); tmem_ld32(tmem_s + 32, sv + 32);
-                    float k[4], ev[4], ms[4];            // of the tile's parts: factor of the scores, V exponent, largest score
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) { const float2 sc = scale_of(c); k[c] = factor(sc.x); ev[c] = sc.y; }
-                    tmem_ld_wait();
-                    float top_s = -INFINITY, top_r = -INFINITY, low_r = INFINITY;
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        ms[c] = largest16(sv + c * kPart) * k[c];
-                        top_s = fmaxf(top_s, ms[c]);
-                        top_r = fmaxf(top_r, ms[c] + ev[c]);
-                        low_r = fminf(low_r, ms[c] + ev[c]);
-                    }
-                    ok = refer(top_s, top_r);
+                    if constexpr (TWO) ok = ways == 2 ? whole(std::integral_constant<int, 2>(), 2 * way, tmem_s, scale_of) : whole(std::integral_constant<int, 4>(), 0, tmem_s, scale_of);
+                    else ok = whole(std::integral_constant<int, 4>(), 0, tmem_s, scale_of);
                     if (!ok) break;
-                    if (__any_sync(0xffffffffu, !(low_r >= R - kFaint))) {
-#pragma unroll
-                        for (int c = 0; c < 4; ++c) ev[c] = exponent(ev[c], ms[c]);
-                    } else {
-#pragma unroll
-                        for (int c = 0; c < 4; ++c) ev[c] -= R;
-                    }
-                    // to tensor memory, over the first half of the row's own scores: 32 keys = 16 columns of pairs per store
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        uint32_t pk[16];
-#pragma unroll
-                        for (int c2 = 0; c2 < 2; ++c2)
-                            probabilities(sv + (2 * h + c2) * kPart, k[2 * h + c2], ev[2 * h + c2], pk + c2 * 8);
-                        tmem_st16(tmem_s + h * 16, pk);
-                    }
-                    tmem_st_wait();
                 } else {
                     // A tile of branches' tokens, or a document's last: columns [lo, hi) of this row, parts [c_lo, c_hi) of the warp's rows; the other parts'
                     // probabilities are zero.
@@ -804,6 +832,7 @@ attn_paged_kernel(const __grid_constant__ Maps maps, const Params p)
                         lo = max(0, my_cs - j * kN);
                         hi = min(kN, my_cs + my_len - j * kN);
                     }
+                    if (ways == 2) { lo = max(lo, way * (kN / 2)); hi = min(hi, (way + 1) * (kN / 2)); }
                     const bool sees = row_valid && hi > lo;
                     const int c_lo = __reduce_min_sync(0xffffffffu, sees ? lo : kN) / kPart;
                     const int c_hi = (__reduce_max_sync(0xffffffffu, sees ? hi : 0) + kPart - 1) / kPart;
@@ -862,14 +891,28 @@ attn_paged_kernel(const __grid_constant__ Maps maps, const Params p)
                 ++qc;
             }
             tc_fence_after();
-            const int g_row = row & (G - 1);
             const int grow_row = u.row0 + b_row;
-            const int hq = u.head * G + g_row;
+            const int hq = u.head * G + (u_row & (G - 1));
             const bool store = row_valid && grow_row < p.a.a.max_rows;
             const bool final_out = u.part_base < 0;
+            // The pipeline's four warps meet (bounded, as all waits are).
+            auto meet = [&]() {
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&misc->meet[x]);
+                return wait_for_warp(&misc->meet[x], meets++ & 1, misc);
+            };
+            float l_row = l, M_row = M;                  // of the row, both ways together
+            if (ways == 2) {
+                misc->way_ml[x][row] = make_float2(M, l);
+                ok = meet();
+                if (!ok) break;
+                const float2 other = misc->way_ml[x][row ^ (kM / 2)];
+                M_row = fmaxf(M, other.x);
+                l_row = (M == -INFINITY ? l : l * ex2(M - M_row)) + (other.x == -INFINITY ? other.y : other.y * ex2(other.x - M_row));
+            }
             // o = O 2^(R - 7 - M) / l, the power in two steps: it may be that of any V scale; a partial result leaves the division out
-            const float two = R == -INFINITY ? 0.f : ex2(0.5f * (R - kUp - M));
-            const float inv = two * (l == 0.f ? 0.f : final_out || l != l ? 1.f / l : 1.f);
+            const float two = R == -INFINITY ? 0.f : ex2(0.5f * (R - kUp - M_row));
+            const float inv = two * (l_row == 0.f ? 0.f : final_out || l_row != l_row ? 1.f / l_row : 1.f);
             const int64_t pr = (static_cast<int64_t>(final_out ? 0 : u.part_base) + u.row_begin + b_row) * p.a.a.g.Hq + hq;
             float* po = p.part_o + pr * D;
             // the accumulator, 32 columns at a time; rolled: the code runs once per unit, out of a cold instruction cache
@@ -890,7 +933,43 @@ attn_paged_kernel(const __grid_constant__ Maps maps, const Params p)
                     if (lane == 0) mbar_arrive(&misc->o_free[x]);
                 }
             };
-            if (final_out) {
+            if (ways == 2) {
+                // 16 columns at a time: the second way's rows hand theirs over in shared memory (column by column), the first way's add and store
+                float* hand = reinterpret_cast<float*>(smem + C::OFF_STAGE + x * 4096) + u_row;
+#pragma unroll 1
+                for (int c0 = 0; c0 < D && ok; c0 += 16) {
+                    uint32_t ov[16];
+                    float acc[16];
+                    tmem_ld16(tmem_o + c0, ov);
+                    tmem_ld_wait();
+#pragma unroll
+                    for (int c = 0; c < 16; ++c) acc[c] = nt > 0 ? two * __uint_as_float(ov[c]) * inv : 0.f;
+                    if (way == 1) {
+#pragma unroll
+                        for (int c = 0; c < 16; ++c) hand[c * (kM / 2)] = acc[c];
+                    }
+                    ok = meet();
+                    if (way == 0 && store && ok) {
+#pragma unroll
+                        for (int c = 0; c < 16; ++c) acc[c] += hand[c * (kM / 2)];
+                        if (final_out) {
+                            uint4* to = reinterpret_cast<uint4*>(p.a.a.o + (static_cast<int64_t>(grow_row) * p.a.a.g.Hq + hq) * D + c0);
+                            to[0] = make_uint4(pack_bf16(acc[0], acc[1]), pack_bf16(acc[2], acc[3]), pack_bf16(acc[4], acc[5]), pack_bf16(acc[6], acc[7]));
+                            to[1] = make_uint4(pack_bf16(acc[8], acc[9]), pack_bf16(acc[10], acc[11]), pack_bf16(acc[12], acc[13]), pack_bf16(acc[14], acc[15]));
+                        } else {
+#pragma unroll
+                            for (int c = 0; c < 16; c += 4) *reinterpret_cast<float4*>(po + c0 + c) = make_float4(acc[c], acc[c + 1], acc[c + 2], acc[c + 3]);
+                        }
+                    }
+                    if (c0 + 16 < D && ok) ok = meet();
+                }
+                if (!ok) break;
+                if (nt > 0) {                            // all TMEM reads of this unit are done
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&misc->o_free[x]);
+                }
+            } else if (final_out) {
 #pragma unroll 1
                 for (int c0 = 0; c0 < D; c0 += 32) {
                     float acc[32];
@@ -929,11 +1008,11 @@ attn_paged_kernel(const __grid_constant__ Maps maps, const Params p)
                     }
                 }
             }
-            if (store) {
+            if (store && way == 0) {
                 if (final_out) {
-                    if (p.a.a.lse) p.a.a.lse[static_cast<int64_t>(grow_row) * p.a.a.g.Hq + hq] = l == 0.f ? -INFINITY : (M + log2f(l)) * kLn2;
+                    if (p.a.a.lse) p.a.a.lse[static_cast<int64_t>(grow_row) * p.a.a.g.Hq + hq] = l_row == 0.f ? -INFINITY : (M_row + log2f(l_row)) * kLn2;
                 } else {
-                    p.part_ml[pr * 2] = M; p.part_ml[pr * 2 + 1] = l;
+                    p.part_ml[pr * 2] = M_row; p.part_ml[pr * 2 + 1] = l_row;
                 }
             }
         }
@@ -970,7 +1049,7 @@ bool make_codes_map(CUtensorMap* m, const void* base, int D, long long rows, int
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int D>
+template <int D, bool TWO>
 int launch_d(const PagedArgs& a)
 {
     using C = Cfg<D>;
@@ -978,7 +1057,7 @@ int launch_d(const PagedArgs& a)
     static std::atomic<bool> attr_set[kMaxDevices];
     const int dev = current_device();
     if (dev < 0 || dev >= kMaxDevices || !attr_set[dev].load(std::memory_order_acquire)) {
-        HPD_CUDA_TRY(cudaFuncSetAttribute(attn_paged_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM));
+        HPD_CUDA_TRY(cudaFuncSetAttribute(attn_paged_kernel<D, TWO>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM));
         if (dev >= 0 && dev < kMaxDevices) attr_set[dev].store(true, std::memory_order_release);
     }
     const hpd_geom& g = a.a.g;
@@ -1002,13 +1081,18 @@ int launch_d(const PagedArgs& a)
     p.part_o = reinterpret_cast<float*>(ws + a.a.lay.off_o);
     p.scale_log2 = g.sm_scale * kLog2e;
     p.G = g.Hq / g.Hkv;
-    attn_paged_kernel<D><<<sm_count(), kThreads, C::SMEM, a.a.stream>>>(maps, p);
+    attn_paged_kernel<D, TWO><<<sm_count(), kThreads, C::SMEM, a.a.stream>>>(maps, p);
     HPD_CUDA_TRY(cudaGetLastError());
     return launch_attn_merge(a.a);
 }
 
 }  // namespace
 
-int launch_attn_paged(const PagedArgs& a) { return a.a.g.D == 128 ? launch_d<128>(a) : launch_d<64>(a); }
+int launch_attn_paged(const PagedArgs& a)
+{
+    const bool two = static_cast<long long>(a.a.max_rows) * (a.a.g.Hq / a.a.g.Hkv) <= static_cast<long long>(a.a.n_docs) * (kM / 2);
+    if (a.a.g.D == 128) return two ? launch_d<128, true>(a) : launch_d<128, false>(a);
+    return two ? launch_d<64, true>(a) : launch_d<64, false>(a);
+}
 
 }  // namespace hpd
