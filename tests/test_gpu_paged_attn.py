@@ -175,6 +175,42 @@ def test_many_units(heads):
     c.check(some=60)
 
 
+@pytest.mark.parametrize("heads", [(8, 2, 128), (4, 1, 64), (2, 2, 128), (8, 1, 64)])
+@pytest.mark.parametrize("P", [16, 64])
+def test_rows_in_two_ways(heads, P):
+    """Enough units that none is halved, few rows on average: units of up to 64 rows and eight tiles or more have their rows twice in the tile, the others
+    once, in the same launch; 64 and 65 rows, 7 and 8 tiles, branches of several tiles and none."""
+    G = heads[0] // heads[1]
+    rng = np.random.default_rng(P)
+    docs = 170 // heads[1]
+    L = rng.integers(440, 700, docs)
+    L[:8] = [448, 449, 512, 511, 1100, 64, 0, 1]
+    n = rng.integers(0, 64 // G // 2, docs)
+    n[:8] = [64 // G, 64 // G + 1, 64 // G, 1, 128 // G, 3, 2, 64 // G]
+    c = Case(heads, P, L, n, 7, seed=P + heads[0], alive=0.9)
+    c.upload()
+    c.attend()
+    c.check(some=60)
+    for d in range(8):                                    # the first documents' first and last row
+        rows = np.flatnonzero(np.repeat(np.arange(docs), n)[c.rows()] == d)
+        q = c.q.float().cpu().numpy().astype(np.float64)
+        for r in rows[[0, -1]] if len(rows) else []:
+            K, V = c.seen(c.rows()[r])
+            o, l = po.attend(q[r], c.g.sm_scale, K, V)
+            bo, bl = po.attention_bounds(q[r], c.g.sm_scale, K, V, o, l)
+            assert np.all(np.abs(c.o[r].float().cpu().numpy() - o) <= bo) and np.all(np.abs(c.lse[r].cpu().numpy() - l) <= bl), (d, r)
+
+
+def test_two_ways_with_scales_of_all_sizes_and_one_visible_half():
+    """Two ways whose references differ by hundreds: pages of very different scales, scores that leave one token, branches in one half of a tile."""
+    for seed, k_exp, v_exp, q_scale in ((31, (118, 122), (60, 190), 1.0), (32, (122, 126), (118, 122), 8.0), (33, (60, 61), (1, 40), 30.0)):
+        c = Case((8, 2, 128), 16, [520 + 7 * (i % 9) for i in range(90)], [1 + i % 5 for i in range(90)], 70, depth=[(13 * i) % 69 for i in range(270)],
+                 seed=seed, k_exp=k_exp, v_exp=v_exp, q_scale=q_scale)
+        c.upload()
+        c.attend()
+        c.check(some=50)
+
+
 @pytest.mark.parametrize("k_exp,v_exp,q_scale", [((60, 61), (100, 160), 1.0), ((105, 122), (60, 190), 1.0), ((120, 121), (1, 40), 30.0),
                                                  ((1, 3), (230, 240), 1e3), ((200, 210), (119, 121), 1e-25)])
 def test_scales_of_all_sizes(k_exp, v_exp, q_scale):
