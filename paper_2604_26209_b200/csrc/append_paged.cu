@@ -122,7 +122,9 @@ __device__ __forceinline__ int page_of(const PageArgs& p, int entry, int64_t ind
 }
 
 // ------------------------------------------------------------------------------------------------
-// One token per sequence: the decode step.  Row r is sequence r's token.
+// One token per sequence: the decode step.  Row r is sequence r's token.  6144 rows (32 / 8 heads of 128, pages of 16): 37 us, 3.8 TB/s; without the
+// rotation 33, without the held codes' rescaling 35, without the angles or the conversions 37: what is left is two batches of loads one after the
+// other per CTA.  (One batch in 256 threads 40.5, six chunks a thread 45.4, ten CTAs an SM 39.1.)
 // ------------------------------------------------------------------------------------------------
 constexpr int kStepThreads = 128, kStepRows = 2, kStepBatch = 3, kStepResident = 8;
 
@@ -204,8 +206,8 @@ append_step_kernel(int Hq /* 0: no queries */, int Hkv, const InvFreq inv_freq, 
             const int slot = s_slot[row], now = max(e8m0_needed(top), was[k]);
             const long long ph = kept ? static_cast<long long>(s_page[row]) * Hkv + (is_v ? head - Hkv : head) : 0;
             uint8_t* codes = (is_v ? p.page_v : p.page_k) + ph * p.page_size * D;
-            // Codes held under a smaller scale, by the whole warp, four loads of 16 in flight: by the head's lanes alone, token by token, a step of
-            // 6144 rows of which a few per cent of the heads need it took 38.5 us.
+            // Codes held under a smaller scale: by the whole warp, four loads of 16 bytes in flight a lane; the head's own lanes would have one
+            // round trip to memory for every token.
             for (unsigned m = __ballot_sync(0xffffffffu, kept && ch == 0 && slot > 0 && now > was[k]); m; m &= m - 1) {
                 const int from = __ffs(m) - 1;
                 uint8_t* at = reinterpret_cast<uint8_t*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(codes), from));
@@ -222,15 +224,16 @@ append_step_kernel(int Hq /* 0: no queries */, int Hkv, const InvFreq inv_freq, 
 
 // ------------------------------------------------------------------------------------------------
 // Any number of tokens per sequence: prompts and chunks.  The rows of a sequence that go into one page are a segment.  A CTA has the
-// segments that begin in its window of 64 rows and takes them in groups of up to 64 rows, for every gridDim.y-th kv head and those heads' queries:
-// the angles of a group's rows are computed once.
+// segments that begin in its window of rows and takes them in groups of up to 64 rows, for every gridDim.y-th kv head and those heads' queries:
+// the angles of a group's rows are computed once.  64 prompts of 2288 tokens (32 / 8 heads of 128): 587 us, 5.6 TB/s.  What few rows cost is a
+// group's chain -- tables, pages, scales, then two round trips per head -- 7.5 us for one prompt, 22.6 for 37 ragged chunks.
 // ------------------------------------------------------------------------------------------------
 constexpr int kTokThreads = 256, kTokRows = 64, kTokQueries = 2;
 template <int D> constexpr int kTokResident = D == 128 ? 3 : 4;       // CTAs of an SM
 
 template <int D>
 __global__ void __launch_bounds__(kTokThreads, kTokResident<D>)
-append_tokens_kernel(int Hq /* 0: no queries */, int Hkv, const InvFreq inv_freq, const PageArgs p)
+append_tokens_kernel(int Hq /* 0: no queries */, int Hkv, int window, const InvFreq inv_freq, const PageArgs p)
 {
     constexpr int HALF = D / 2, CH = D / 16;
     constexpr int B = kTokRows * CH / kTokThreads;   // chunk pairs of one head's keys (or values) a thread holds
@@ -238,12 +241,12 @@ append_tokens_kernel(int Hq /* 0: no queries */, int Hkv, const InvFreq inv_freq
     __shared__ int s_seg[kTokRows], s_slot[kTokRows];                        // per row: its segment in the group, its place in the page
     __shared__ int g_page[kTokRows], g_held[kTokRows];                       // per segment: page (-1: none), tokens that it held
     __shared__ int g_top[2][2][kTokRows], g_was[2][2][kTokRows];             // per parity of the head, K / V and segment: largest magnitude, scale of before
-    __shared__ uint32_t s_starts[2];
+    __shared__ uint32_t s_starts[4];
     __shared__ int s_end;
     const int n = min(*p.n_rows, p.max_rows);
     const int P = p.page_size, G = Hq / Hkv, q_shift = 31 - __clz(max(G, 1) * CH);
-    const int64_t lo = static_cast<int64_t>(blockIdx.x) * kTokRows;
-    const int end = static_cast<int>(min(lo + kTokRows, static_cast<int64_t>(n)));
+    const int64_t lo = static_cast<int64_t>(blockIdx.x) * window;
+    const int end = static_cast<int>(min(lo + window, static_cast<int64_t>(n)));
     const int t0 = threadIdx.x;
     for (int r = static_cast<int>(min(lo, static_cast<int64_t>(n))); r < end;) {
         // ---- the group's rows: where they go, where segments begin ----
@@ -253,7 +256,7 @@ append_tokens_kernel(int Hq /* 0: no queries */, int Hkv, const InvFreq inv_freq
         int entry = -1, slot = 0, stop = 0;
         int64_t index = 0;
         bool start = false;
-        if (t0 < kTokRows) {
+        if (t0 < 2 * kTokRows) {
             const int row = r + t0;
             if (row < n) {
                 const int seq = p.row_seq[row];
@@ -273,24 +276,26 @@ append_tokens_kernel(int Hq /* 0: no queries */, int Hkv, const InvFreq inv_freq
             if ((t0 & 31) == 0) s_starts[t0 >> 5] = starts;
         }
         __syncthreads();
-        const uint64_t starts = s_starts[0] | static_cast<uint64_t>(s_starts[1]) << 32;
-        if (!(starts & 1)) {                         // the window begins inside a segment, which another one has
-            r = starts ? r + __ffsll(static_cast<long long>(starts)) - 1 : r + kTokRows;
-            continue;
-        }
-        if (t0 < kTokRows) {
-            const int seg = __popcll(starts & (~0ull >> (63 - t0))) - 1;
-            s_seg[t0] = seg; s_slot[t0] = slot;
-            if (starts >> t0 & 1) {
+        // Behind the rows of a segment that another window has: 64 rows from the first segment on that begins here.
+        const uint64_t near = s_starts[0] | static_cast<uint64_t>(s_starts[1]) << 32, far = s_starts[2] | static_cast<uint64_t>(s_starts[3]) << 32;
+        const int skip = near ? __ffsll(static_cast<long long>(near)) - 1 : kTokRows;
+        const uint64_t starts = !near ? 0 : skip ? near >> skip | far << (64 - skip) : near;
+        r += skip;
+        const int t = t0 - skip;
+        if (t >= 0 && t < kTokRows) {
+            const int seg = __popcll(starts & (~0ull >> (63 - t))) - 1;
+            s_seg[t] = seg; s_slot[t] = slot;
+            if (starts >> t & 1) {
                 int page = -1;
                 if (entry >= 0) page = page_of(p, entry, index, blockIdx.y == 0);
                 else if (blockIdx.y == 0 && p.dev_status) atomicOr(p.dev_status, HPD_S_BAD_TABLE);
                 g_page[seg] = page; g_held[seg] = page < 0 ? 0 : slot;
-                if (r + t0 < end && stop - r <= kTokRows) atomicMax(&s_end, stop);       // later ones are another window's
+                if (r + t < end && stop - r <= kTokRows) atomicMax(&s_end, stop);        // later ones are another window's
             }
         }
         __syncthreads();
-        const int rows = s_end - r;                  // whole segments only: the first one at least
+        const int rows = s_end - r;                  // whole segments only
+        if (rows <= 0) break;                        // none begins in the window
         const int segs = __popcll(starts & (~0ull >> (64 - rows)));
         if (p.pos_id)
             for (int i = t0; i < rows * HALF; i += kTokThreads) {
@@ -403,11 +408,17 @@ int launch_append_paged(const hpd_geom& g, const AppendPagedArgs& a)
         if (wide) append_step_kernel<128><<<grid, kStepThreads, 0, a.stream>>>(Hq, g.Hkv, f, p);
         else append_step_kernel<64><<<grid, kStepThreads, 0, a.stream>>>(Hq, g.Hkv, f, p);
     } else {
-        // few rows: the heads of a window go to several CTAs, up to two waves of three an SM
-        const unsigned windows = (static_cast<unsigned>(a.max_rows) + kTokRows - 1) / kTokRows;
-        const dim3 grid(windows, std::min<unsigned>(g.Hkv, std::max(1u, 3u * sm_count() / windows)));
-        if (wide) append_tokens_kernel<128><<<grid, kTokThreads, 0, a.stream>>>(Hq, g.Hkv, f, p);
-        else append_tokens_kernel<64><<<grid, kTokThreads, 0, a.stream>>>(Hq, g.Hkv, f, p);
+        // A window's segments should be one group: windows of 64 less a page.  Pages of 64: 32 (half of the windows begin no segment and end at once), but
+        // 64 while every window and head has a CTA at the same time.  In us with windows of 64 / 48 / 32 rows: 37 ragged chunks in pages of 16
+        // 26.8 / 22.7 / 23.2, of 32 26.8 / 28.5 / 23.5; 64 prompts of 2288 tokens in pages of 16 647 / 588 / 617, of 32 635 / 627 / 611, of 64
+        // 615 / 595 / 587; one prompt in pages of 64 7.5 / 8.2 / 9.6.
+        const unsigned resident = 4u * sm_count(), rows = static_cast<unsigned>(a.max_rows);
+        const unsigned all = static_cast<unsigned>(kTokRows), window = a.page_size <= 16 ? 48 : a.page_size > 32 && (rows + all - 1) / all * g.Hkv <= resident ? all : 32;
+        const unsigned windows = (rows + window - 1) / window;
+        // few rows: the heads of a window go to several CTAs
+        const dim3 grid(windows, std::min<unsigned>(g.Hkv, std::max(1u, resident / windows)));
+        if (wide) append_tokens_kernel<128><<<grid, kTokThreads, 0, a.stream>>>(Hq, g.Hkv, static_cast<int>(window), f, p);
+        else append_tokens_kernel<64><<<grid, kTokThreads, 0, a.stream>>>(Hq, g.Hkv, static_cast<int>(window), f, p);
     }
     HPD_CUDA_TRY(cudaGetLastError());
     return HPD_OK;

@@ -12,11 +12,20 @@
 //                exponent of its probabilities there: no instruction per element for either.
 //   O += P V     two warps of each pipeline widen V tiles from e4m3 to fp16 (exact) in shared memory; P is fp16 with its largest elements
 //                between 2^7 and 2^15, so that what is flushed is below 2^-31 of them.  They zero what lies behind a tile's last
-//                token, NaN codes included, and write the two terms of Q.
+//                token; they also fetch Q and write its two terms in its place.
 //
 // Two references per row.  With s the scaled score (log2) and e the V exponent of its page, R >= s + e - 8 is what the products P V are
 // relative to (rescaled when it grows by more than 8), M >= s is what the sum is relative to.  A part of 16 columns whose products
 // stay below 2^-60 of R takes part in the sum alone: its probabilities are raised to there, where fp16 flushes them.
+//
+// NaN.  The pages of a document are all its rows' in any case.  Branches share tiles, and 0 * NaN would reach the others: a NaN among a branch's V
+// codes is zeroed and noted, and its rows become NaN in the epilogue; one among its K codes stays in its own columns, which others' rows mask.
+//
+// What bounds it.  64 prompts of 24 documents (500 tokens, 96 branches on average): 165 us for 72.7 us of bytes at the copy rate, 146 us in bf16 over
+// an unpaged cache of twice the bytes.  The copies and matrix products alone take 105 us (a product of 128 x 64 x 16 or 32 takes the tensor core 48 to
+// 64 cycles here whatever its type: 16 of them per tile); the softmax of a tile is a chain of 1.9 k cycles for its warp, 2.3 k with both
+// pipelines' on the SM's issue slots (40 % used), which is why units of few rows are taken apart (ways_of); a unit's turn costs 8 k cycles
+// (Q fetched and split 5 k, epilogue 3 k), of which the other pipeline covers about half.
 //
 // Warps: 0 / 3 scheduler and copies of pipeline 0 / 1, 1 / 2 MMA issuers, 4-7 / 8-11 softmax, 12-13 / 14-15 conversion.
 // TMEM columns as in hpd_attn_decode: S0 [0,64) S1 [64,128) O [128,256) of a pipeline, P over the first half of its scores.
@@ -117,18 +126,6 @@ struct Misc {
 };
 static_assert(sizeof(Misc) <= 8192, "misc block");
 
-// Bounded wait: false once two to four seconds (2^32 cycles and more) have passed or another thread of the CTA has given up.  Short on purpose: it stands
-// at some forty places, and the kernel's code competes for the instruction cache (138 KB of it cost 8 % against 80).
-__device__ __forceinline__ uint32_t clock_high() { uint32_t t; asm volatile("mov.u32 %0, %%clock_hi;" : "=r"(t)); return t; }
-__device__ __forceinline__ bool wait_for(unsigned long long* bar, uint32_t parity, Misc* misc) {
-    if (mbar_try_wait(bar, parity)) return true;
-    return mbar_wait(bar, parity, misc);
-}
-// all lanes wait; the result is made warp-uniform so that warp-collective instructions stay converged
-__device__ __forceinline__ bool wait_for_warp(unsigned long long* bar, uint32_t parity, Misc* misc) {
-    return __all_sync(0xffffffffu, wait_for(bar, parity, misc));
-}
-
 // tcgen05.mma on two operands of e4m3 codes in shared memory (descriptors' low and high words)
 __device__ __forceinline__ void tc_mma_codes(uint32_t d_tmem, uint32_t a_lo, uint32_t a_hi, uint32_t b_lo, uint32_t b_hi, uint32_t idesc, uint32_t accumulate) {
     asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\t"
@@ -150,6 +147,9 @@ __device__ __forceinline__ uint32_t idesc_wide(int N) { return idesc_codes(N) | 
 // In a kernel of its own, for steps whose documents have 64 rows or fewer on average: the code for both in one cost the others 4 %.
 constexpr int kTwoTiles = 8;
 template <bool TWO> __device__ __forceinline__ int ways_of(int nrows, int nt) { return TWO && nrows <= kM / 2 && nt >= kTwoTiles ? 2 : 1; }
+
+// power of two that a V scale byte stands for; NaN for NaN
+__device__ __forceinline__ float v_exponent(int byte) { return byte == 255 ? __uint_as_float(0x7fffffffu) : static_cast<float>(byte - 127); }
 
 struct Unit { int nt, np, stot, head, key_count, part_base, row_begin, nb, row0; };
 __device__ __forceinline__ Unit read_unit(const UnitDesc& d) {
@@ -222,220 +222,216 @@ attn_paged_kernel(const __grid_constant__ Maps maps, const Params p)
         if (n_units == 0) {
             if (lane == 0) { d.nt = -1; mbar_arrive(&misc->desc_full[x]); }
         } else {
-        constexpr int kStatic = 6;
-        const bool spread = n_units < 4 * 2 * static_cast<int>(gridDim.x);
-        const uint32_t first_dynamic = static_cast<uint32_t>(kStatic) * 2u * gridDim.x;
-        auto next = [&](int i) {                                     // the pipeline's i-th unit
-            uint32_t t = 0;
-            if (i < kStatic) {
-                const uint32_t j = spread ? blockIdx.x + static_cast<uint32_t>(x) * gridDim.x : 2u * blockIdx.x + static_cast<uint32_t>(x);
-                t = (((i & 1) && alternate) ? 2u * gridDim.x - 1u - j : j) + static_cast<uint32_t>(i) * 2u * gridDim.x;
-            } else {
-                if (lane == 0) t = atomicAdd(ticket, 1u);
-                t = __shfl_sync(0xffffffffu, t, 0) + first_dynamic;
-            }
-            return static_cast<int>(min(t, static_cast<uint32_t>(n_units)));
-        };
-        auto item_of = [&](int w) {
-            const int i = min(w, n_units - 1);
-            WorkItem it = p.work[i / Hkv / halves];
-            if (TWO && halves == 2) {
-                const int first = (it.row_count + 1) / 2;
-                if (i / Hkv & 1) { it.row_begin += first; it.row_count -= first; } else { it.row_count = first; }
-                if (it.row_count == 0) { it.key_count = 0; it.with_suffix = 0; }      // a single row: nothing is left for the other half
-            }
-            return it;
-        };
-        // ---- the links of a unit's chain: row tables and page numbers; branches' pages; scales ----
-        int len[kRounds], page[kRounds], ks[kRounds], vs[kRounds];   // per branch; page: slot, then page, then first row of its codes
-        int bad;                                                     // a table entry out of range
-        // per lane: one of 32 pages of the document: its number (-2: not needed), then first row of its codes (-1: none) and scale bytes
-        int id, row, sk, sv;
-        auto branches_of = [&](int w, const WorkItem& it) { return w < n_units && it.with_suffix ? it.row_count : 0; };
-        auto page_id = [&](const WorkItem& it, int i) {
-            const int at = (it.key_begin >> shift) + i;
-            if (i << shift >= it.key_count) return -2;
-            return at < p.a.pages_per_doc ? p.a.page_table[static_cast<int64_t>(it.doc) * p.a.pages_per_doc + at] : -1;
-        };
-        auto page_scales = [&](int id_, int head, int& row_, int& sk_, int& sv_) {
-            row_ = -1; sk_ = 127; sv_ = 127;
-            if (id_ == -2) return;
-            if (id_ < 0 || id_ >= p.a.n_pages) { sk_ = 255; bad = 1; return; }      // NaN for the document's rows
-            const int64_t ph = static_cast<int64_t>(id_) * Hkv + head;
-            row_ = static_cast<int>(ph << shift);
-            sk_ = p.a.scale_k[ph]; sv_ = p.a.scale_v[ph];
-        };
-        auto link_rows = [&](int w, const WorkItem& it) {
-            const int nb = branches_of(w, it);
-#pragma unroll
-            for (int r = 0; r < kRounds; ++r) {
-                const int b = lane + 32 * r;
-                len[r] = 0; page[r] = -1;
-                if (b < nb) {
-                    len[r] = p.a.a.suffix_len[it.doc_row + it.row_begin + b];
-                    page[r] = p.a.a.active_slot[it.doc_row + it.row_begin + b];
+            constexpr int kStatic = 6;
+            const bool spread = n_units < 4 * 2 * static_cast<int>(gridDim.x);
+            const uint32_t first_dynamic = static_cast<uint32_t>(kStatic) * 2u * gridDim.x;
+            auto next = [&](int i) {                                     // the pipeline's i-th unit
+                uint32_t t = 0;
+                if (i < kStatic) {
+                    const uint32_t j = spread ? blockIdx.x + static_cast<uint32_t>(x) * gridDim.x : 2u * blockIdx.x + static_cast<uint32_t>(x);
+                    t = (((i & 1) && alternate) ? 2u * gridDim.x - 1u - j : j) + static_cast<uint32_t>(i) * 2u * gridDim.x;
+                } else {
+                    if (lane == 0) t = atomicAdd(ticket, 1u);
+                    t = __shfl_sync(0xffffffffu, t, 0) + first_dynamic;
                 }
-            }
-            id = w < n_units ? page_id(it, lane) : -2;
-        };
-        auto link_pages = [&]() {
-            bad = 0;
-#pragma unroll
-            for (int r = 0; r < kRounds; ++r) {
-                const int n = len[r] + p.a.a.suffix_extra;
-                len[r] = n < 0 ? 0 : n > p.a.a.g.suffix_cap ? p.a.a.g.suffix_cap : n;
-                if (page[r] < 0) len[r] = 0;
-                if (len[r] > 0) page[r] = page[r] < p.a.a.n_slots ? p.a.slot_page[page[r]] : -1;
-            }
-        };
-        auto link_scales = [&](int w) {
-            const int head = w % Hkv;
-#pragma unroll
-            for (int r = 0; r < kRounds; ++r) {
-                ks[r] = vs[r] = 127;
-                if (len[r] > 0) {
-                    if (page[r] < 0 || page[r] >= p.a.n_branch_pages) {
-                        bad = 1; len[r] = 0;
-                    } else {
-                        const int64_t ph = static_cast<int64_t>(page[r]) * Hkv + head;
-                        ks[r] = p.a.branch_scale_k[ph]; vs[r] = p.a.branch_scale_v[ph];
-                        page[r] = static_cast<int>(ph * p.a.a.g.suffix_cap);
-                    }
-                }
-            }
-            page_scales(id, head, row, sk, sv);
-        };
-        auto report = [&]() { if (__any_sync(0xffffffffu, bad) && lane == 0 && status) atomicOr(status, HPD_S_BAD_TABLE); };
-        // unit ui is w0, the next one w1; before the first there is one without tiles, so that the links stand in one place
-        int w0 = n_units, w1 = next(0);
-        WorkItem it1 = item_of(w1), it0 = it1;
-        int st = 0, sc = 0;                                          // stages of the next tile's copies, and the parities of their barriers
-        uint32_t k_par = 1, c_par = 1;
-        bool ok = true;
-        for (int ui = -1; ok; ++ui) {
-            int nt = 0, ns = 0, np = 0, head = 0, row0 = 0, key_count = 0, carry = 0, nb = 0;
-            int cs[kRounds], blen[kRounds], brow[kRounds];           // per branch: first column, tokens, first row of its codes
-            float2* scales = misc->page_scale[x][ui & 1];
-            auto put_scales = [&](int batch, int k, int v) {
-                scales[(batch & 1) * 32 + lane] = make_float2(e8m0_value(k), v == 255 ? __uint_as_float(0x7fffffffu) : static_cast<float>(v - 127));
+                return static_cast<int>(min(t, static_cast<uint32_t>(n_units)));
             };
-            int cur_row = -1, nxt_id = -2, nxt_row = -1, nxt_sk = 127, nxt_sv = 127;       // this unit's batch of 32 pages, and the next
-            if (ui >= 0) {
-            // ---- scan and publish unit ui ----
-            if (ui >= 1) {
-                ok = wait_for_warp(&misc->desc_empty[x], (ui - 1) & 1, misc);
-                if (!ok) break;
-            }
-            const bool live = w0 < n_units;
-            report();
-            nb = branches_of(w0, it0);
-#pragma unroll
-            for (int r = 0; r < kRounds; ++r) {
-                cs[r] = 0; blen[r] = 0; brow[r] = 0;
-                if (32 * r < nb) {
-                    const int b = lane + 32 * r;
-                    const int occ = (len[r] + C::PAD - 1) / C::PAD * C::PAD;
-                    int incl = occ;
-#pragma unroll
-                    for (int s = 1; s < 32; s <<= 1) {
-                        const int v = __shfl_up_sync(0xffffffffu, incl, s);
-                        if (lane >= s) incl += v;
-                    }
-                    cs[r] = carry + incl - occ; blen[r] = len[r]; brow[r] = page[r];
-                    d.cs[b] = static_cast<uint16_t>(cs[r]);
-                    d.len[b] = static_cast<uint16_t>(len[r]);
-                    d.ks[b] = static_cast<uint8_t>(ks[r]);
-                    d.vs[b] = static_cast<uint8_t>(vs[r]);
-                    carry += __shfl_sync(0xffffffffu, incl, 31);
+            auto item_of = [&](int w) {
+                const int i = min(w, n_units - 1);
+                WorkItem it = p.work[i / Hkv / halves];
+                if (TWO && halves == 2) {
+                    const int first = (it.row_count + 1) / 2;
+                    if (i / Hkv & 1) { it.row_begin += first; it.row_count -= first; } else { it.row_count = first; }
+                    if (it.row_count == 0) { it.key_count = 0; it.with_suffix = 0; }      // a single row: nothing is left for the other half
                 }
-            }
-            ns = (carry + kN - 1) / kN; np = live ? (it0.key_count + kN - 1) / kN : 0;
-            nt = live ? ns + np : -1; head = w0 % Hkv; row0 = it0.doc_row + it0.row_begin; key_count = it0.key_count;
-            if (lane == 0) {
-                d.nt = nt; d.np = np; d.stot = carry; d.head = head; d.key_count = key_count; d.part_base = it0.part_base;
-                d.row_begin = it0.row_begin; d.nb = it0.row_count; d.row0 = row0; d.nb_cached = nb;
-            }
-            put_scales(0, sk, sv);
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&misc->desc_full[x]);
-            if (!live) break;
-            if (np > 0 || ns > 0)                                    // q on its way into L2: its tile is released late in the unit before
-                if (elect_one())
-                    for (int h = 0; h < D / 64; ++h) tma_prefetch_4d(&maps.q, h * 64, 0, head, row0);
-            __syncwarp();
-            cur_row = row;
-            nxt_id = page_id(it0, 32 + lane);
-            }
-            const int w2 = next(ui + 2);
-            const WorkItem it2 = item_of(w2);
-            link_rows(w1, it1);
-            for (int t = 0; t < max(nt, 2) && ok; ++t) {
-                if (t < nt) {
-                uint8_t* kt = k_ring + st * C::KV_BYTES;
-                uint8_t* ct = c_ring + sc * C::KV_BYTES;
-                unsigned long long *kf = &misc->k_full[x][st], *cf = &misc->c_full[x][sc];
-                ok = wait_for_warp(&misc->k_empty[x][st], k_par, misc) && wait_for_warp(&misc->c_empty[x][sc], c_par, misc);
-                if (!ok) break;
-                if (t < ns) {
-                    // pieces of the branches that fall into the tile; a box has the exact height of the piece
-                    const int c_lo = t * kN, c_hi = min(carry, c_lo + kN);
-                    int mine = 0;
+                return it;
+            };
+            // ---- the links of a unit's chain: row tables and page numbers; branches' pages; scales ----
+            int len[kRounds], page[kRounds], ks[kRounds], vs[kRounds];   // per branch; page: slot, then page, then first row of its codes
+            int bad;                                                     // a table entry out of range
+            // per lane: one of 32 pages of the document: its number (-2: not needed), then first row of its codes (-1: none) and scale bytes
+            int id, row, sk, sv;
+            auto branches_of = [&](int w, const WorkItem& it) { return w < n_units && it.with_suffix ? it.row_count : 0; };
+            auto page_id = [&](const WorkItem& it, int i) {
+                const int at = (it.key_begin >> shift) + i;
+                if (i << shift >= it.key_count) return -2;
+                return at < p.a.pages_per_doc ? p.a.page_table[static_cast<int64_t>(it.doc) * p.a.pages_per_doc + at] : -1;
+            };
+            auto page_scales = [&](int id_, int head, int& row_, int& sk_, int& sv_) {
+                row_ = -1; sk_ = 127; sv_ = 127;
+                if (id_ == -2) return;
+                if (id_ < 0 || id_ >= p.a.n_pages) { sk_ = 255; bad = 1; return; }      // NaN for the document's rows
+                const int64_t ph = static_cast<int64_t>(id_) * Hkv + head;
+                row_ = static_cast<int>(ph << shift);
+                sk_ = p.a.scale_k[ph]; sv_ = p.a.scale_v[ph];
+            };
+            auto link_rows = [&](int w, const WorkItem& it) {
+                const int nb = branches_of(w, it);
 #pragma unroll
-                    for (int r = 0; r < kRounds; ++r)
-                        if (32 * r < nb) mine += max(0, min(cs[r] + blen[r], c_hi) - max(cs[r], c_lo));
-                    const uint32_t bytes = __reduce_add_sync(0xffffffffu, mine) * D;
-                    if (lane == 0) { mbar_expect_tx(kf, bytes); mbar_expect_tx(cf, bytes); }
+                for (int r = 0; r < kRounds; ++r) {
+                    const int b = lane + 32 * r;
+                    len[r] = 0; page[r] = -1;
+                    if (b < nb) {
+                        len[r] = p.a.a.suffix_len[it.doc_row + it.row_begin + b];
+                        page[r] = p.a.a.active_slot[it.doc_row + it.row_begin + b];
+                    }
+                }
+                id = w < n_units ? page_id(it, lane) : -2;
+            };
+            auto link_pages = [&]() {
+                bad = 0;
 #pragma unroll
-                    for (int r = 0; r < kRounds; ++r) {
-                        if (32 * r >= nb) break;
-                        const int lo = max(cs[r], c_lo);
-                        int n = min(cs[r] + blen[r], c_hi) - lo, from = brow[r] + (lo - cs[r]), col = lo - c_lo;
-                        if (n > 0) bulk_load(ct + col * D, p.a.branch_v + static_cast<int64_t>(from) * D, cf, static_cast<uint32_t>(n) * D);
-                        while (n > 0) {
-                            const int hb = min(n, 16);
-                            tma_load_2d(kt + col * D, &maps.branch[hb - 1], kf, 0, from);
-                            from += hb; col += hb; n -= hb;
+                for (int r = 0; r < kRounds; ++r) {
+                    const int n = len[r] + p.a.a.suffix_extra;
+                    len[r] = n < 0 ? 0 : n > p.a.a.g.suffix_cap ? p.a.a.g.suffix_cap : n;
+                    if (page[r] < 0) len[r] = 0;
+                    if (len[r] > 0) page[r] = page[r] < p.a.a.n_slots ? p.a.slot_page[page[r]] : -1;
+                }
+            };
+            auto link_scales = [&](int w) {
+                const int head = w % Hkv;
+#pragma unroll
+                for (int r = 0; r < kRounds; ++r) {
+                    ks[r] = vs[r] = 127;
+                    if (len[r] > 0) {
+                        if (page[r] < 0 || page[r] >= p.a.n_branch_pages) {
+                            bad = 1; len[r] = 0;
+                        } else {
+                            const int64_t ph = static_cast<int64_t>(page[r]) * Hkv + head;
+                            ks[r] = p.a.branch_scale_k[ph]; vs[r] = p.a.branch_scale_v[ph];
+                            page[r] = static_cast<int>(ph * p.a.a.g.suffix_cap);
                         }
                     }
-                } else {
-                    // the lanes that hold the tile's pages copy them
-                    const int tp = t - ns, in_batch = tp & (per_batch - 1);
-                    if (tp > 0 && in_batch == 0) {                   // the next 32 pages; ask for the ones behind them
-                        cur_row = nxt_row;
-                        nxt_id = page_id(it0, (tp / per_batch + 1) * 32 + lane);
+                }
+                page_scales(id, head, row, sk, sv);
+            };
+            auto report = [&]() { if (__any_sync(0xffffffffu, bad) && lane == 0 && status) atomicOr(status, HPD_S_BAD_TABLE); };
+            // unit ui is w0, the next one w1; before the first there is one without tiles, so that the links stand in one place
+            int w0 = n_units, w1 = next(0);
+            WorkItem it1 = item_of(w1), it0 = it1;
+            int st = 0, sc = 0;                                          // stages of the next tile's copies, and the parities of their barriers
+            uint32_t k_par = 1, c_par = 1;
+            bool ok = true;
+            for (int ui = -1; ok; ++ui) {
+                int nt = 0, ns = 0, np = 0, head = 0, row0 = 0, key_count = 0, carry = 0, nb = 0;
+                int cs[kRounds], blen[kRounds], brow[kRounds];           // per branch: first column, tokens, first row of its codes
+                float2* scales = misc->page_scale[x][ui & 1];
+                auto put_scales = [&](int batch, int k, int v) {
+                    scales[(batch & 1) * 32 + lane] = make_float2(e8m0_value(k), v_exponent(v));
+                };
+                int cur_row = -1, nxt_id = -2, nxt_row = -1, nxt_sk = 127, nxt_sv = 127;       // this unit's batch of 32 pages, and the next
+                if (ui >= 0) {
+                    // ---- scan and publish unit ui ----
+                    if (ui >= 1) {
+                        ok = mbar_wait_warp(&misc->desc_empty[x], (ui - 1) & 1, misc);
+                        if (!ok) break;
                     }
-                    const int pages = (min(kN, key_count - tp * kN) + P - 1) >> shift, j = lane - in_batch * per_tile;
-                    const bool copies = j >= 0 && j < pages && cur_row >= 0;
-                    const uint32_t bytes = static_cast<uint32_t>(__popc(__ballot_sync(0xffffffffu, copies))) * P * D;
-                    if (lane == 0) { mbar_expect_tx(kf, bytes); mbar_expect_tx(cf, bytes); }
-                    if (copies) {
-                        tma_load_2d(kt + j * P * D, &maps.page, kf, 0, cur_row);
-                        bulk_load(ct + j * P * D, p.a.page_v + static_cast<int64_t>(cur_row) * D, cf, static_cast<uint32_t>(P) * D);
+                    const bool live = w0 < n_units;
+                    report();
+                    nb = branches_of(w0, it0);
+#pragma unroll
+                    for (int r = 0; r < kRounds; ++r) {
+                        cs[r] = 0; blen[r] = 0; brow[r] = 0;
+                        if (32 * r < nb) {
+                            const int b = lane + 32 * r;
+                            const int occ = (len[r] + C::PAD - 1) / C::PAD * C::PAD;
+                            int incl = occ;
+#pragma unroll
+                            for (int s = 1; s < 32; s <<= 1) {
+                                const int v = __shfl_up_sync(0xffffffffu, incl, s);
+                                if (lane >= s) incl += v;
+                            }
+                            cs[r] = carry + incl - occ; blen[r] = len[r]; brow[r] = page[r];
+                            d.cs[b] = static_cast<uint16_t>(cs[r]);
+                            d.len[b] = static_cast<uint16_t>(len[r]);
+                            d.ks[b] = static_cast<uint8_t>(ks[r]);
+                            d.vs[b] = static_cast<uint8_t>(vs[r]);
+                            carry += __shfl_sync(0xffffffffu, incl, 31);
+                        }
                     }
-                    if (in_batch == 1) {
-                        const int was = bad;
-                        bad = 0;
-                        page_scales(nxt_id, head, nxt_row, nxt_sk, nxt_sv);
-                        report();
-                        bad = was;
+                    ns = (carry + kN - 1) / kN; np = live ? (it0.key_count + kN - 1) / kN : 0;
+                    nt = live ? ns + np : -1; head = w0 % Hkv; row0 = it0.doc_row + it0.row_begin; key_count = it0.key_count;
+                    if (lane == 0) {
+                        d.nt = nt; d.np = np; d.stot = carry; d.head = head; d.key_count = key_count; d.part_base = it0.part_base;
+                        d.row_begin = it0.row_begin; d.nb = it0.row_count; d.row0 = row0; d.nb_cached = nb;
                     }
-                    // The next batch's scales, over those of the batch before this one: the softmax is at most NK + 2 tiles behind, so it has left it.
-                    if (in_batch == per_batch - 1 && tp + 1 < np) {
-                        put_scales(tp / per_batch + 1, nxt_sk, nxt_sv);
+                    put_scales(0, sk, sv);
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&misc->desc_full[x]);
+                    if (!live) break;
+                    cur_row = row;
+                    nxt_id = page_id(it0, 32 + lane);
+                }
+                const int w2 = next(ui + 2);
+                const WorkItem it2 = item_of(w2);
+                link_rows(w1, it1);
+                for (int t = 0; t < max(nt, 2) && ok; ++t) {
+                    if (t < nt) {
+                        uint8_t* kt = k_ring + st * C::KV_BYTES;
+                        uint8_t* ct = c_ring + sc * C::KV_BYTES;
+                        unsigned long long *kf = &misc->k_full[x][st], *cf = &misc->c_full[x][sc];
+                        ok = mbar_wait_warp(&misc->k_empty[x][st], k_par, misc) && mbar_wait_warp(&misc->c_empty[x][sc], c_par, misc);
+                        if (!ok) break;
+                        if (t < ns) {
+                            // pieces of the branches that fall into the tile; a box has the exact height of the piece
+                            const int c_lo = t * kN, c_hi = min(carry, c_lo + kN);
+                            int mine = 0;
+#pragma unroll
+                            for (int r = 0; r < kRounds; ++r)
+                                if (32 * r < nb) mine += max(0, min(cs[r] + blen[r], c_hi) - max(cs[r], c_lo));
+                            const uint32_t bytes = __reduce_add_sync(0xffffffffu, mine) * D;
+                            if (lane == 0) { mbar_expect_tx(kf, bytes); mbar_expect_tx(cf, bytes); }
+#pragma unroll
+                            for (int r = 0; r < kRounds; ++r) {
+                                if (32 * r >= nb) break;
+                                const int lo = max(cs[r], c_lo);
+                                int n = min(cs[r] + blen[r], c_hi) - lo, from = brow[r] + (lo - cs[r]), col = lo - c_lo;
+                                if (n > 0) bulk_load(ct + col * D, p.a.branch_v + static_cast<int64_t>(from) * D, cf, static_cast<uint32_t>(n) * D);
+                                while (n > 0) {
+                                    const int hb = min(n, 16);
+                                    tma_load_2d(kt + col * D, &maps.branch[hb - 1], kf, 0, from);
+                                    from += hb; col += hb; n -= hb;
+                                }
+                            }
+                        } else {
+                            // the lanes that hold the tile's pages copy them
+                            const int tp = t - ns, in_batch = tp & (per_batch - 1);
+                            if (tp > 0 && in_batch == 0) {                   // the next 32 pages; ask for the ones behind them
+                                cur_row = nxt_row;
+                                nxt_id = page_id(it0, (tp / per_batch + 1) * 32 + lane);
+                            }
+                            const int pages = (min(kN, key_count - tp * kN) + P - 1) >> shift, j = lane - in_batch * per_tile;
+                            const bool copies = j >= 0 && j < pages && cur_row >= 0;
+                            const uint32_t bytes = static_cast<uint32_t>(__popc(__ballot_sync(0xffffffffu, copies))) * P * D;
+                            if (lane == 0) { mbar_expect_tx(kf, bytes); mbar_expect_tx(cf, bytes); }
+                            if (copies) {
+                                tma_load_2d(kt + j * P * D, &maps.page, kf, 0, cur_row);
+                                bulk_load(ct + j * P * D, p.a.page_v + static_cast<int64_t>(cur_row) * D, cf, static_cast<uint32_t>(P) * D);
+                            }
+                            if (in_batch == 1) {
+                                const int was = bad;
+                                bad = 0;
+                                page_scales(nxt_id, head, nxt_row, nxt_sk, nxt_sv);
+                                report();
+                                bad = was;
+                            }
+                            // The next batch's scales, over those of the batch before this one: the softmax is at most NK + 2 tiles behind, so it has left it.
+                            if (in_batch == per_batch - 1 && tp + 1 < np) {
+                                put_scales(tp / per_batch + 1, nxt_sk, nxt_sv);
+                                __syncwarp();
+                                if (lane == 0) mbar_arrive(&misc->batch_full[x]);
+                            }
+                        }
                         __syncwarp();
-                        if (lane == 0) mbar_arrive(&misc->batch_full[x]);
+                        if (++st == C::NK) { st = 0; k_par ^= 1; }
+                        if (++sc == C::NC) { sc = 0; c_par ^= 1; }
                     }
+                    if (t == 0) link_pages();
+                    if (t == 1) link_scales(w1);
                 }
-                __syncwarp();
-                if (++st == C::NK) { st = 0; k_par ^= 1; }
-                if (++sc == C::NC) { sc = 0; c_par ^= 1; }
-                }
-                if (t == 0) link_pages();
-                if (t == 1) link_scales(w1);
+                if (!ok) break;
+                w0 = w1; w1 = w2; it0 = it1; it1 = it2;
             }
-            if (!ok) break;
-            w0 = w1; w1 = w2; it0 = it1; it1 = it2;
-        }
         }
     } else if (warp < 3) {
         // ================================ MMA issuers (one per pipeline) =============================
@@ -451,7 +447,7 @@ attn_paged_kernel(const __grid_constant__ Maps maps, const Params p)
             const uint32_t tmem_s = tmem + x * kColPipe + kColS, tmem_o = tmem + x * kColPipe + kColO;
             const uint32_t idesc_pv = idesc_wide(D);
             for (uint32_t ui = 0; ok; ++ui) {
-                ok = wait_for(&misc->desc_full[x], ui & 1, misc);
+                ok = mbar_wait(&misc->desc_full[x], ui & 1, misc);
                 if (!ok) break;
                 const Unit u = read_unit(misc->desc[x]);
                 mbar_arrive(&misc->desc_empty[x]);
@@ -466,14 +462,14 @@ attn_paged_kernel(const __grid_constant__ Maps maps, const Params p)
                     else if (j == nt - 1) c = last_p;
                     return (c + 15) >> 4;
                 };
-                ok = wait_for(&misc->q_full[x], qc & 1, misc);
+                ok = mbar_wait(&misc->q_full[x], qc & 1, misc);
                 ++qc;
                 auto issue_qk = [&](int j) {
                     const uint32_t kt = tiles + j;
                     const int ks = kt % C::NK, sb = kt & 1;
                     const uint32_t idesc = idesc_codes(cols16(j) << 4);
                     const uint32_t k_lo = k_lo0 + ks * (C::KV_BYTES >> 4);
-                    if (!wait_for(&misc->k_full[x][ks], (kt / C::NK) & 1, misc)) return false;
+                    if (!mbar_wait(&misc->k_full[x][ks], (kt / C::NK) & 1, misc)) return false;
                     tc_fence_after();
                     // k-steps of 32 codes; the low terms of q are a tile (D = 128) or half a row (D = 64) behind the high ones
 #pragma unroll
@@ -498,8 +494,8 @@ attn_paged_kernel(const __grid_constant__ Maps maps, const Params p)
                     const uint32_t v_lo = v_lo0 + vs * (C::WIDE_BYTES >> 4);
                     const int nk = cols16(j);
                     const uint32_t acc0 = j >= 1;
-                    if (j == 0 && qc > 1) ok = wait_for(&misc->o_free[x], (qc - 2) & 1, misc);       // the epilogue of the unit before has read O
-                    if (ok) ok = wait_for(&misc->pv_full[x][pb], (vt >> 1) & 1, misc);
+                    if (j == 0 && qc > 1) ok = mbar_wait(&misc->o_free[x], (qc - 2) & 1, misc);       // the epilogue of the unit before has read O
+                    if (ok) ok = mbar_wait(&misc->pv_full[x][pb], (vt >> 1) & 1, misc);
                     if (!ok) break;
                     tc_fence_after();
 #pragma unroll
@@ -522,7 +518,7 @@ attn_paged_kernel(const __grid_constant__ Maps maps, const Params p)
         uint32_t tiles = 0, qc = 0;
         bool ok = true;
         for (uint32_t ui = 0; ok; ++ui) {
-            ok = wait_for_warp(&misc->desc_full[x], ui & 1, misc);
+            ok = mbar_wait_warp(&misc->desc_full[x], ui & 1, misc);
             if (!ok) break;
             const UnitDesc& d = misc->desc[x];
             const Unit u = read_unit(d);
@@ -537,7 +533,7 @@ attn_paged_kernel(const __grid_constant__ Maps maps, const Params p)
             constexpr int LANES = D / 16, ROWS = 32 / LANES, BATCH = 2;
             const int nrows = u.nb * G, ways = ways_of<TWO>(nrows, u.nt), part = lane % LANES;
             if (half == 0) {
-                ok = wait_for_warp(&misc->q_empty[x], (qc & 1) ^ 1, misc);
+                ok = mbar_wait_warp(&misc->q_empty[x], (qc & 1) ^ 1, misc);
                 if (!ok) break;
                 if (elect_one()) {
                     mbar_expect_tx(&misc->q_raw[x], C::Q_BYTES);
@@ -545,7 +541,7 @@ attn_paged_kernel(const __grid_constant__ Maps maps, const Params p)
                 }
                 __syncwarp();
             }
-            ok = wait_for_warp(&misc->q_raw[x], qc & 1, misc);
+            ok = mbar_wait_warp(&misc->q_raw[x], qc & 1, misc);
             if (!ok) break;
             if (lane < 4) misc->nan_branch[x][qc & 1][half][lane] = 0u;
             for (int r0 = half * (BATCH * ROWS); r0 < nrows; r0 += 2 * BATCH * ROWS) {
@@ -607,9 +603,9 @@ attn_paged_kernel(const __grid_constant__ Maps maps, const Params p)
                 const int rows = min(kN, own ? u.stot - t * kN : u.key_count - (t - ns) * kN);       // what lies behind is zero
                 uint8_t* src = c_ring + sc * C::KV_BYTES;
                 uint8_t* dst = v_ring + sv * C::WIDE_BYTES;
-                ok = wait_for_warp(&misc->c_full[x][sc], (tiles / C::NC) & 1, misc);
+                ok = mbar_wait_warp(&misc->c_full[x][sc], (tiles / C::NC) & 1, misc);
                 if (!ok) break;
-                ok = wait_for_warp(&misc->v_empty[x][sv], ((tiles / C::NV) & 1) ^ 1, misc);
+                ok = mbar_wait_warp(&misc->v_empty[x][sv], ((tiles / C::NV) & 1) ^ 1, misc);
                 if (!ok) break;
                 // pieces of 8 codes: 16 bytes of fp16 each, one below another for a thread (rows of 128 bytes, exchanged like q's)
                 constexpr int PIECES = D / 8, STEP = 64 / PIECES, BATCH_V = 8;
@@ -680,7 +676,7 @@ attn_paged_kernel(const __grid_constant__ Maps maps, const Params p)
         uint32_t pw = 0, qc = 0, batches = 0, meets = 0; // tiles done (S read, P written), units with tiles, batches of pages beyond the first, meetings
         bool ok = true;
         for (uint32_t unit_idx = 0; ok; ++unit_idx) {
-            ok = wait_for_warp(&misc->desc_full[x], unit_idx & 1, misc);
+            ok = mbar_wait_warp(&misc->desc_full[x], unit_idx & 1, misc);
             if (!ok) break;
             const UnitDesc& d = misc->desc[x];
             const Unit u = read_unit(d);
@@ -689,7 +685,7 @@ attn_paged_kernel(const __grid_constant__ Maps maps, const Params p)
             const int b_row = u_row >> g_shift;          // its branch inside the unit
             const bool cached = b_row < d.nb_cached;
             const int my_cs = cached ? d.cs[b_row] : 0, my_len = cached ? d.len[b_row] : 0;
-            const float my_k = e8m0_value(cached ? d.ks[b_row] : 127), my_e = !cached ? 0.f : d.vs[b_row] == 255 ? __uint_as_float(0x7fffffffu) : static_cast<float>(d.vs[b_row] - 127);
+            const float my_k = e8m0_value(cached ? d.ks[b_row] : 127), my_e = cached ? v_exponent(d.vs[b_row]) : 0.f;
             __syncwarp();
             if (lane == 0) mbar_arrive(&misc->desc_empty[x]);
             if (u.nt < 0) break;
@@ -698,7 +694,7 @@ attn_paged_kernel(const __grid_constant__ Maps maps, const Params p)
             const bool warp_active = quad * 32 - way * (kM / 2) < nrows;
             float q_factor = 0.f;
             if (nt > 0) {
-                ok = wait_for_warp(&misc->q_full[x], qc & 1, misc);
+                ok = mbar_wait_warp(&misc->q_full[x], qc & 1, misc);
                 if (!ok) break;
                 // rows behind the unit's last hold anything: their scores are made zero, or they would have the warp rescale O in every tile
                 q_factor = row_valid ? misc->q_factor[x][row] * p.scale_log2 : 0.f;
@@ -715,7 +711,7 @@ attn_paged_kernel(const __grid_constant__ Maps maps, const Params p)
                 const bool grow = top_r > R + kRescaleSlack || top_s > M + kRescaleSlack;
                 if (__any_sync(0xffffffffu, grow)) {
                     // O must be rescaled: wait until the previous P V product has landed in TMEM.  (In a unit's first tile all rows are fresh.)
-                    if (!wait_for_warp(&misc->v_empty[x][(pw - 1) % C::NV], ((pw - 1) / C::NV) & 1, misc)) return false;
+                    if (!mbar_wait_warp(&misc->v_empty[x][(pw - 1) % C::NV], ((pw - 1) / C::NV) & 1, misc)) return false;
                     tc_fence_after();
                     const float r_new = grow ? fmaxf(R, top_r) : R, m_new = grow ? fmaxf(M, top_s) : M;
                     const float f = grow ? ex2(R - r_new) : 1.f;
@@ -791,7 +787,7 @@ attn_paged_kernel(const __grid_constant__ Maps maps, const Params p)
                     low_r = fminf(low_r, ms[c] + ev[c]);
                 }
                 if (!refer(top_s, top_r)) return false;
-                if (__any_sync(0xffffffffu, !(low_r >= R - kFaint))) {
+                if (__any_sync(0xffffffffu, row_valid && !(low_r >= R - kFaint))) {
 #pragma unroll
                     for (int c = 0; c < PARTS; ++c) ev[c] = exponent(ev[c], ms[c]);
                 } else {
@@ -820,18 +816,20 @@ attn_paged_kernel(const __grid_constant__ Maps maps, const Params p)
                 const uint32_t tmem_s = tmem_s0 + pb * kN;
                 // K scale and V exponent of the tile's c-th part
                 const int first_page = (j - ns) << (6 - shift);
-                auto scale_of = [&](int c) { return j < ns ? make_float2(my_k, my_e) : misc->page_scale[x][unit_idx & 1][(first_page + (c * kPart >> shift)) & 63]; };
+                auto scale_of = [&](int c) {
+                    return j < ns ? make_float2(my_k, my_e) : misc->page_scale[x][unit_idx & 1][(first_page + (c * kPart >> shift)) & 63];
+                };
                 if (j > ns && (first_page & 31) == 0) {  // the next 32 pages
-                    ok = wait_for_warp(&misc->batch_full[x], batches & 1, misc);
+                    ok = mbar_wait_warp(&misc->batch_full[x], batches & 1, misc);
                     if (!ok) break;
                     ++batches;
                 }
-                ok = wait_for_warp(&misc->s_full[x][pb], (pw >> 1) & 1, misc);
+                ok = mbar_wait_warp(&misc->s_full[x][pb], (pw >> 1) & 1, misc);
                 if (!ok) break;
                 tc_fence_after();
                 if (!warp_active) {                      // no rows: nobody reads its probabilities' products
                 } else if (j >= ns && j < j_full) {
-                    if constexpr (TWO) ok = ways == 2 ? whole(std::integral_constant<int, 2>(), 2 * way, tmem_s, scale_of) : whole(std::integral_constant<int, 4>(), 0, tmem_s, scale_of);
+                    if (TWO && ways == 2) ok = whole(std::integral_constant<int, 2>(), 2 * way, tmem_s, scale_of);
                     else ok = whole(std::integral_constant<int, 4>(), 0, tmem_s, scale_of);
                     if (!ok) break;
                 } else {
@@ -894,7 +892,7 @@ attn_paged_kernel(const __grid_constant__ Maps maps, const Params p)
 
             // ------------------------------------ epilogue ------------------------------------
             if (nt > 0) {                                // the unit's last P V product has landed (and the P tile is free)
-                ok = wait_for_warp(&misc->o_full[x], qc & 1, misc);
+                ok = mbar_wait_warp(&misc->o_full[x], qc & 1, misc);
                 if (!ok) break;
                 const volatile uint32_t* nan = &misc->nan_branch[x][qc & 1][0][0];
                 if (ns > 0 && (nan[b_row >> 5] | nan[4 + (b_row >> 5)]) >> (b_row & 31) & 1) l = __uint_as_float(0x7fffffffu);
@@ -909,7 +907,7 @@ attn_paged_kernel(const __grid_constant__ Maps maps, const Params p)
             auto meet = [&]() {
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&misc->meet[x]);
-                return wait_for_warp(&misc->meet[x], meets++ & 1, misc);
+                return mbar_wait_warp(&misc->meet[x], meets++ & 1, misc);
             };
             float l_row = l, M_row = M;                  // of the row, both ways together
             if (ways == 2) {

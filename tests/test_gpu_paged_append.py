@@ -115,6 +115,32 @@ def test_token_form(heads, P, rotate):
     assert bool((q_rot[T if rotate else 0:] == 7).all())
 
 
+@pytest.mark.parametrize("P", [64, 50, 33, 32, 16, 7])
+def test_token_form_of_many_rows(P):
+    """More windows of rows than are on the GPU at a time; pages that end anywhere in them; one row, whole pages and long chunks side by side."""
+    g = geom((16, 8, 64))
+    rng = np.random.default_rng(100 + P)
+    new = np.concatenate([rng.integers(1, 900, 10), [1, 1, 1, P, 2 * P, 64, 65, 63], rng.integers(0, 3, 30)])
+    new = np.concatenate([new, [5400 - new.sum()]]) if new.sum() < 5400 else new
+    rng.shuffle(new)
+    held = rng.integers(0, 2 * P, len(new))
+    per = int((-(-(new + held) // P)).max())
+    n_seqs, T = len(new), int(new.sum())
+    table = np.full((n_seqs, per), -1)
+    need = -(-(new + held) // P)
+    pages = rng.permutation(int(need.sum()))
+    for s, a in enumerate(np.cumsum(need) - need):
+        table[s, :need[s]] = pages[a:a + need[s]]
+    c = Case(g, len(pages), P, table, T, seed=P + 5, spread=2)
+    start = np.concatenate([[0], np.cumsum(new)])
+    row_seq = np.repeat(np.arange(n_seqs), new)
+    index = held[row_seq] + np.arange(T) - start[row_seq]
+    pos = rng.integers(0, 9000, T)
+    q_rot = torch.full_like(c.q, 7.0)
+    c.B.hpd_append_paged(g, n_seqs, T, i32([T]), i32(row_seq), i32(start), None, i32(held), c.cache, i32(pos), c.q, q_rot, c.k, c.v, c.status)
+    c.check(row_seq, index, pos, q_rot)
+
+
 def test_keys_only_with_rotation():
     g = geom((8, 2, 128))
     c = Case(g, 8, 16, np.arange(8)[:, None], 8, seed=3)
