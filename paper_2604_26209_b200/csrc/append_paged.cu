@@ -225,8 +225,10 @@ append_step_kernel(int Hq /* 0: no queries */, int Hkv, const InvFreq inv_freq, 
 // ------------------------------------------------------------------------------------------------
 // Any number of tokens per sequence: prompts and chunks.  The rows of a sequence that go into one page are a segment.  A CTA has the
 // segments that begin in its window of rows and takes them in groups of up to 64 rows, for every gridDim.y-th kv head and those heads' queries:
-// the angles of a group's rows are computed once.  64 prompts of 2288 tokens (32 / 8 heads of 128): 587 us, 5.6 TB/s.  What few rows cost is a
-// group's chain -- tables, pages, scales, then two round trips per head -- 7.5 us for one prompt, 22.6 for 37 ragged chunks.
+// the angles of a group's rows are computed once, each thread those of one frequency (its frequency and the rows' position IDs fetched with the
+// tables: 586 -> 575 us and 22.6 -> 18.5; from the table of parameters lane by lane and from memory row by row they were a third of a small call).
+// 64 prompts of 2288 tokens (32 / 8 heads of 128, pages of 64): 575 us, 5.7 TB/s.  What few rows cost is a group's chain -- tables, pages, scales,
+// then two round trips per head: 7.5 us for one prompt, 18.5 for 37 ragged chunks.
 // ------------------------------------------------------------------------------------------------
 constexpr int kTokThreads = 256, kTokRows = 64, kTokQueries = 2;
 template <int D> constexpr int kTokResident = D == 128 ? 3 : 4;       // CTAs of an SM
@@ -238,7 +240,7 @@ append_tokens_kernel(int Hq /* 0: no queries */, int Hkv, int window, const InvF
     constexpr int HALF = D / 2, CH = D / 16;
     constexpr int B = kTokRows * CH / kTokThreads;   // chunk pairs of one head's keys (or values) a thread holds
     __shared__ float cs[kTokRows][HALF], sn[kTokRows][HALF];
-    __shared__ int s_seg[kTokRows], s_slot[kTokRows];                        // per row: its segment in the group, its place in the page
+    __shared__ int s_seg[kTokRows], s_slot[kTokRows], s_pos[kTokRows];       // per row: its segment in the group, its place in the page, its position ID
     __shared__ int g_page[kTokRows], g_held[kTokRows];                       // per segment: page (-1: none), tokens that it held
     __shared__ int g_top[2][2][kTokRows], g_was[2][2][kTokRows];             // per parity of the head, K / V and segment: largest magnitude, scale of before
     __shared__ uint32_t s_starts[4];
@@ -248,6 +250,7 @@ append_tokens_kernel(int Hq /* 0: no queries */, int Hkv, int window, const InvF
     const int64_t lo = static_cast<int64_t>(blockIdx.x) * window;
     const int end = static_cast<int>(min(lo + window, static_cast<int64_t>(n)));
     const int t0 = threadIdx.x;
+    const double freq = p.pos_id ? inv_freq.f[t0 % HALF] : 0.;               // of the angles that this thread computes
     for (int r = static_cast<int>(min(lo, static_cast<int64_t>(n))); r < end;) {
         // ---- the group's rows: where they go, where segments begin ----
         __syncthreads();                             // the tables of the group before have been used
@@ -283,6 +286,7 @@ append_tokens_kernel(int Hq /* 0: no queries */, int Hkv, int window, const InvF
         r += skip;
         const int t = t0 - skip;
         if (t >= 0 && t < kTokRows) {
+            if (p.pos_id && r + t < n) s_pos[t] = p.pos_id[r + t];
             const int seg = __popcll(starts & (~0ull >> (63 - t))) - 1;
             s_seg[t] = seg; s_slot[t] = slot;
             if (starts >> t & 1) {
@@ -298,10 +302,7 @@ append_tokens_kernel(int Hq /* 0: no queries */, int Hkv, int window, const InvF
         if (rows <= 0) break;                        // none begins in the window
         const int segs = __popcll(starts & (~0ull >> (64 - rows)));
         if (p.pos_id)
-            for (int i = t0; i < rows * HALF; i += kTokThreads) {
-                const int t = i / HALF, a = i % HALF;
-                rotary_angle(p.pos_id[r + t], inv_freq.f[a], cs[t][a], sn[t][a]);
-            }
+            for (int t = t0 / HALF; t < rows; t += kTokThreads / HALF) rotary_angle(s_pos[t], freq, cs[t][t0 % HALF], sn[t][t0 % HALF]);
         // ---- head by head: while the keys and values are on their way, the head's queries ----
         for (int h = blockIdx.y, par = 0; h < Hkv; h += gridDim.y, par ^= 1) {
             Chunk k[B], v[B];
@@ -408,12 +409,12 @@ int launch_append_paged(const hpd_geom& g, const AppendPagedArgs& a)
         if (wide) append_step_kernel<128><<<grid, kStepThreads, 0, a.stream>>>(Hq, g.Hkv, f, p);
         else append_step_kernel<64><<<grid, kStepThreads, 0, a.stream>>>(Hq, g.Hkv, f, p);
     } else {
-        // A window's segments should be one group: windows of 64 less a page.  Pages of 64: 32 (half of the windows begin no segment and end at once), but
-        // 64 while every window and head has a CTA at the same time.  In us with windows of 64 / 48 / 32 rows: 37 ragged chunks in pages of 16
-        // 26.8 / 22.7 / 23.2, of 32 26.8 / 28.5 / 23.5; 64 prompts of 2288 tokens in pages of 16 647 / 588 / 617, of 32 635 / 627 / 611, of 64
-        // 615 / 595 / 587; one prompt in pages of 64 7.5 / 8.2 / 9.6.
-        const unsigned resident = 4u * sm_count(), rows = static_cast<unsigned>(a.max_rows);
-        const unsigned all = static_cast<unsigned>(kTokRows), window = a.page_size <= 16 ? 48 : a.page_size > 32 && (rows + all - 1) / all * g.Hkv <= resident ? all : 32;
+        // A window's segments should be one group of up to 64 rows: windows of 48, but 64 for large pages while every window and head has a CTA at the
+        // same time.  In us with windows of 64 / 48 / 32 rows: 37 ragged chunks in pages of 16 24.6 / 18.5 / 21.8, of 32 23.3 / 23.0 / 20.7, of 64
+        // 24.7 / 25.5 / 32.6; 64 prompts of 2288 tokens in pages of 16 572 / 560 / 596, of 32 576 / 572 / 593, of 64 590 / 575 / 571; one
+        // prompt in pages of 64 7.6 / 8.1 / 10.1.
+        const unsigned resident = 4u * sm_count(), rows = static_cast<unsigned>(a.max_rows), all = static_cast<unsigned>(kTokRows);
+        const unsigned window = a.page_size > 32 && (rows + all - 1) / all * g.Hkv <= resident ? all : 48;
         const unsigned windows = (rows + window - 1) / window;
         // few rows: the heads of a window go to several CTAs
         const dim3 grid(windows, std::min<unsigned>(g.Hkv, std::max(1u, resident / windows)));
