@@ -413,11 +413,16 @@ int launch_append_paged(const hpd_geom& g, const AppendPagedArgs& a)
         // same time.  In us with windows of 64 / 48 / 32 rows: 37 ragged chunks in pages of 16 24.6 / 18.5 / 21.8, of 32 23.3 / 23.0 / 20.7, of 64
         // 24.7 / 25.5 / 32.6; 64 prompts of 2288 tokens in pages of 16 572 / 560 / 596, of 32 576 / 572 / 593, of 64 590 / 575 / 571; one
         // prompt in pages of 64 7.6 / 8.1 / 10.1.
-        const unsigned resident = 4u * sm_count(), rows = static_cast<unsigned>(a.max_rows), all = static_cast<unsigned>(kTokRows);
-        const unsigned window = a.page_size > 32 && (rows + all - 1) / all * g.Hkv <= resident ? all : 48;
+        const unsigned resident = static_cast<unsigned>(wide ? kTokResident<128> : kTokResident<64>) * sm_count();
+        const unsigned rows = static_cast<unsigned>(a.max_rows), all = static_cast<unsigned>(kTokRows), heads = static_cast<unsigned>(g.Hkv);
+        const unsigned window = a.page_size > 32 && (rows + all - 1) / all * heads <= resident ? all : 48;
         const unsigned windows = (rows + window - 1) / window;
-        // few rows: the heads of a window go to several CTAs
-        const dim3 grid(windows, std::min<unsigned>(g.Hkv, std::max(1u, resident / windows)));
+        // The heads of a window go to several CTAs, each with tables and angles of its own: as many as fit the GPU at once, and no more than three heads to
+        // a CTA until the windows alone are several rounds of it.  Prompts of 2288 tokens, 1 / 2 / 4 / 8 / 16 / 32 / 64 of them, in us: one CTA
+        // 57 / 62 / 94 / 113 / 194 / 317 / 574, two 35 / 42 / 64 / 102 / 167 / 311 / 575, three 29 / 35 / 55 / 88 / 161 / 307 / 586,
+        // four 25 / 33 / 62 / 94 / 170 / 320 / 609, eight 20.6 / 35 / 59 / 102 / 190 / 367 / 710.
+        const unsigned fit = std::max(1u, resident / windows), few = windows < 6 * resident ? (heads + 2) / 3 : 1;
+        const dim3 grid(windows, std::min(heads, std::max(fit, few)));
         if (wide) append_tokens_kernel<128><<<grid, kTokThreads, 0, a.stream>>>(Hq, g.Hkv, static_cast<int>(window), f, p);
         else append_tokens_kernel<64><<<grid, kTokThreads, 0, a.stream>>>(Hq, g.Hkv, static_cast<int>(window), f, p);
     }
