@@ -337,6 +337,7 @@ int hpd_append_paged(const hpd_geom* geom /*host*/, int n_seqs, int max_rows, co
  * of its rows.  Scores, softmax and sums are held in fp32; probabilities are rounded to fp16, codes enter the products exactly.
  *   q [max_rows, Hq, D] bf16 (rotated); doc_page [n_docs, pages_per_doc], slot_page [n_slots] int32 (dev); tables and workspace from
  *   hpd_build_meta (active_slot, suffix_len, ...); suffix_includes_new, o, lse as hpd_attn_decode.  Documents may share pages.
+ *   The workspace holds the step's plan and the call's partial results: calls that share one follow each other in a stream, as with hpd_attn_decode.
  *   What lies in a page behind its last token, NaN included, has no influence.  A NaN code in a document's key or value reaches the rows of that document
  *   alone, one of a branch that branch's rows alone (all of their elements); a row whose q holds an infinity or NaN is NaN.
  *   A document's page out of range sets HPD_S_BAD_TABLE and makes that document's rows NaN; so does a document longer than

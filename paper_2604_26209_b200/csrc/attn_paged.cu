@@ -21,11 +21,12 @@
 // NaN.  The pages of a document are all its rows' in any case.  Branches share tiles, and 0 * NaN would reach the others: a NaN among a branch's V
 // codes is zeroed and noted, and its rows become NaN in the epilogue; one among its K codes stays in its own columns, which others' rows mask.
 //
-// What bounds it.  64 prompts of 24 documents (500 tokens, 96 branches on average): 165 us for 72.7 us of bytes at the copy rate, 146 us in bf16 over
-// an unpaged cache of twice the bytes.  The copies and matrix products alone take 105 us (a product of 128 x 64 x 16 or 32 takes the tensor core 48 to
-// 64 cycles here whatever its type: 16 of them per tile); the softmax of a tile is a chain of 1.9 k cycles for its warp, 2.3 k with both
-// pipelines' on the SM's issue slots (40 % used), which is why units of few rows are taken apart (ways_of); a unit's turn costs 8 k cycles
-// (Q fetched and split 5 k, epilogue 3 k), of which the other pipeline covers about half.
+// What bounds it.  64 prompts (256 documents of 512 tokens with 24 branches each, 32 / 8 heads of 128): 165 us for 72.7 us of bytes at the copy rate
+// and 146 us of hpd_attn_decode over an unpaged bf16 cache of twice the bytes; 192 documents of 1024 to 4096 tokens with 12 branches: 290 for 165,
+// and 369 in bf16 (after a second of it, at the clock that the power cap leaves, 178 and 342).  The copies and matrix products alone take 105 of the 165 us
+// (a product of 128 x 64 x 16 or 32 takes the tensor core 48 to 64 cycles here whatever its type: 12 of them per tile); the softmax of a tile
+// is a chain of 1.9 k cycles for its warp, 2.3 k with both pipelines' on the SM's issue slots (41 % used), which is why units of few rows
+// are taken apart (ways_of); a unit's turn costs 8 k cycles (Q fetched and split 5 k, epilogue 3 k), of which the other pipeline covers about half.
 //
 // Warps: 0 / 3 scheduler and copies of pipeline 0 / 1, 1 / 2 MMA issuers, 4-7 / 8-11 softmax, 12-13 / 14-15 conversion.
 // TMEM columns as in hpd_attn_decode: S0 [0,64) S1 [64,128) O [128,256) of a pipeline, P over the first half of its scores.
