@@ -213,3 +213,58 @@ def test_two_layers_share_tables_and_workspace():
     torch.cuda.synchronize()
     for c, (o, l) in zip((a, b), alone):
         assert torch.equal(c.o.view(torch.int16), o.view(torch.int16)) and torch.equal(c.lse, l)
+
+
+def test_two_batches_at_once():
+    """Batches with caches and workspaces of their own, their steps as graphs on two streams at the same time: the bits of each alone."""
+    from paper_2604_26209_b200 import runtime
+    made = []
+    for i, cfg in enumerate((synth.config_main(n_prompts=4, seed=8), synth.config_custom("ragged", 8, 2, 64, 1e4, 12, [0, 1, 70, 3000, 129], [3, 1, 20, 33, 0], 12, alive_frac=0.7))):
+        t = synth.make_tensors(cfg)
+        pb = runtime.PagedBatch(cfg, t, (64, 16)[i])
+        pb.build_meta()
+        n = pb.tables()["n_active"]
+        act = pb.tables()["active_slot"][:n]
+        pb.set_step_inputs(t["q"][act], t["k_new"][act], t["v_new"][act])
+        pb.step()
+        torch.cuda.synchronize()
+        made.append((pb, pb.capture_step(), torch.cuda.Stream(), pb.o.clone(), pb.lse.clone()))
+        pb.o.zero_()
+        pb.lse.zero_()
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for pb, graph, stream, _, _ in made:
+            with torch.cuda.stream(stream):
+                graph.replay()
+    torch.cuda.synchronize()
+    for pb, _, _, o, lse in made:
+        assert torch.equal(pb.o.view(torch.int16), o.view(torch.int16)) and torch.equal(pb.lse, lse) and pb.status() == 0
+
+
+def test_bf16_and_paged_calls_take_turns_on_one_workspace():
+    """The two attentions on the tables, the plan and the ticket counter of one step, one after the other: the bits of each alone."""
+    from paper_2604_26209_b200 import runtime
+    s = synth.config_main(n_prompts=1, seed=9)
+    t = synth.make_tensors(s)
+    pb, db = runtime.PagedBatch(s, t), runtime.DeviceBatch(s, t)
+    db.meta = pb.db.meta
+    pb.build_meta()
+    n = pb.tables()["n_active"]
+    act = pb.tables()["active_slot"][:n]
+    for b in (pb, db):
+        b.set_step_inputs(t["q"][act], t["k_new"][act], t["v_new"][act])
+    db.rope()
+    db.kv_append()
+    db.attn(True)
+    pb.append()
+    pb.attn()
+    torch.cuda.synchronize()
+    want = [x.clone() for x in (db.o, pb.o, pb.lse)]
+    for _ in range(10):
+        pb.attn()
+        db.attn(True)
+    pb.attn()
+    torch.cuda.synchronize()
+    for x, y in zip((db.o, pb.o, pb.lse), want):
+        assert torch.equal(x, y)
+    assert pb.status() == 0
