@@ -607,6 +607,8 @@ attn_paged_kernel(const __grid_constant__ Maps maps, const Params p)
                 ok = mbar_wait_warp(&misc->c_full[x][sc], (tiles / C::NC) & 1, misc);
                 if (!ok) break;
                 ok = mbar_wait_warp(&misc->v_empty[x][sv], ((tiles / C::NV) & 1) ^ 1, misc);
+                // the epilogue of the unit before may be using the tile's memory
+                if (TWO && ok && t == 0 && qc > 0) ok = mbar_wait_warp(&misc->o_free[x], (qc - 1) & 1, misc);
                 if (!ok) break;
                 // pieces of 8 codes: 16 bytes of fp16 each, one below another for a thread (rows of 128 bytes, exchanged like q's)
                 constexpr int PIECES = D / 8, STEP = 64 / PIECES, BATCH_V = 8;
@@ -943,41 +945,42 @@ attn_paged_kernel(const __grid_constant__ Maps maps, const Params p)
                 }
             };
             if (ways == 2) {
-                // 16 columns at a time: the second way's rows hand theirs over in shared memory (column by column), the first way's add and store
-                float* hand = reinterpret_cast<float*>(smem + C::OFF_STAGE + x * 4096) + u_row;
+                // Each way finishes half of the columns: it hands the other's over, 32 at a time and column by column, in the memory of the widened V
+                // tile, which the conversion leaves alone until O is free.  (16 columns at a time from the second way to the first, in the staging
+                // memory, took 5.7 k cycles of the unit.)
+                static_assert(C::NV * C::WIDE_BYTES == 2 * 32 * (kM / 2) * 4, "two ways' 32 columns of 64 rows");
+                float* hand = reinterpret_cast<float*>(smem + C::OFF_V + x * C::NV * C::WIDE_BYTES) + u_row;
+                float *mine = hand + way * 32 * (kM / 2), *theirs = hand + (way ^ 1) * 32 * (kM / 2);
 #pragma unroll 1
-                for (int c0 = 0; c0 < D && ok; c0 += 16) {
-                    uint32_t ov[16];
-                    float acc[16];
-                    tmem_ld16(tmem_o + c0, ov);
+                for (int c0 = 0; c0 < D / 2 && ok; c0 += 32) {
+                    uint32_t ov[32];
+                    tmem_ld32(tmem_o + (way ^ 1) * (D / 2) + c0, ov);
                     tmem_ld_wait();
 #pragma unroll
-                    for (int c = 0; c < 16; ++c) acc[c] = nt > 0 ? two * __uint_as_float(ov[c]) * inv : 0.f;
-                    if (way == 1) {
-#pragma unroll
-                        for (int c = 0; c < 16; ++c) hand[c * (kM / 2)] = acc[c];
-                    }
+                    for (int c = 0; c < 32; ++c) mine[c * (kM / 2)] = two * __uint_as_float(ov[c]) * inv;
+                    const int own = way * (D / 2) + c0;
+                    tmem_ld32(tmem_o + own, ov);
                     ok = meet();
-                    if (way == 0 && store && ok) {
+                    tmem_ld_wait();
+                    if (!ok) break;
+                    float acc[32];
 #pragma unroll
-                        for (int c = 0; c < 16; ++c) acc[c] += hand[c * (kM / 2)];
-                        if (final_out) {
-                            uint4* to = reinterpret_cast<uint4*>(p.a.a.o + (static_cast<int64_t>(grow_row) * p.a.a.g.Hq + hq) * D + c0);
-                            to[0] = make_uint4(pack_bf16(acc[0], acc[1]), pack_bf16(acc[2], acc[3]), pack_bf16(acc[4], acc[5]), pack_bf16(acc[6], acc[7]));
-                            to[1] = make_uint4(pack_bf16(acc[8], acc[9]), pack_bf16(acc[10], acc[11]), pack_bf16(acc[12], acc[13]), pack_bf16(acc[14], acc[15]));
-                        } else {
+                    for (int c = 0; c < 32; ++c) acc[c] = two * __uint_as_float(ov[c]) * inv + theirs[c * (kM / 2)];
+                    if (store && final_out) {
+                        uint4* to = reinterpret_cast<uint4*>(p.a.a.o + (static_cast<int64_t>(grow_row) * p.a.a.g.Hq + hq) * D + own);
 #pragma unroll
-                            for (int c = 0; c < 16; c += 4) *reinterpret_cast<float4*>(po + c0 + c) = make_float4(acc[c], acc[c + 1], acc[c + 2], acc[c + 3]);
-                        }
+                        for (int c = 0; c < 32; c += 8)
+                            to[c / 8] = make_uint4(pack_bf16(acc[c], acc[c + 1]), pack_bf16(acc[c + 2], acc[c + 3]), pack_bf16(acc[c + 4], acc[c + 5]), pack_bf16(acc[c + 6], acc[c + 7]));
+                    } else if (store) {
+#pragma unroll
+                        for (int c = 0; c < 32; c += 4) *reinterpret_cast<float4*>(po + own + c) = make_float4(acc[c], acc[c + 1], acc[c + 2], acc[c + 3]);
                     }
-                    if (c0 + 16 < D && ok) ok = meet();
+                    if (c0 + 32 < D / 2) ok = meet();
                 }
                 if (!ok) break;
-                if (nt > 0) {                            // all TMEM reads of this unit are done
-                    tc_fence_before();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(&misc->o_free[x]);
-                }
+                tc_fence_before();                       // all TMEM reads of this unit are done (it has tiles), and what was handed over has been read
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&misc->o_free[x]);
             } else if (final_out) {
 #pragma unroll 1
                 for (int c0 = 0; c0 < D; c0 += 32) {
