@@ -143,7 +143,7 @@ __device__ __forceinline__ uint32_t idesc_codes(int N) { return (1u << 4) | (sta
 __device__ __forceinline__ uint32_t idesc_wide(int N) { return idesc_codes(N) | (1u << 16); }
 
 // Units of up to 64 rows and at least kTwoTiles tiles have their rows twice in the tile: rows 0-63 take the first half of every tile's keys, rows 64-127 the
-// second, each with references and sums of their own; the epilogue adds them up, 3 k cycles more.  A tile's softmax is then half as long, and that is
+// second, each with references and sums of their own; the epilogue adds them up.  A tile's softmax is then half as long, and that is
 // what most of a tile's time is (192 documents of 1024 to 4096 tokens, 12 branches of 4 heads: 337 -> 285 us).
 // In a kernel of its own, for steps whose documents have 64 rows or fewer on average: the code for both in one cost the others 4 %.
 constexpr int kTwoTiles = 8;
