@@ -266,20 +266,31 @@ attn_paged_kernel(const __grid_constant__ Maps maps, const Params p)
                 row_ = static_cast<int>(ph << shift);
                 sk_ = p.a.scale_k[ph]; sv_ = p.a.scale_v[ph];
             };
-            auto link_rows = [&](int w, const WorkItem& it) {
+            int first_row;                                               // the document's, as the tables passed have it
+            auto row_tables = [&](int w, const WorkItem& it, int row0) {
                 const int nb = branches_of(w, it);
 #pragma unroll
                 for (int r = 0; r < kRounds; ++r) {
                     const int b = lane + 32 * r;
                     len[r] = 0; page[r] = -1;
                     if (b < nb) {
-                        len[r] = p.a.a.suffix_len[it.doc_row + it.row_begin + b];
-                        page[r] = p.a.a.active_slot[it.doc_row + it.row_begin + b];
+                        len[r] = p.a.a.suffix_len[row0 + it.row_begin + b];
+                        page[r] = p.a.a.active_slot[row0 + it.row_begin + b];
                     }
                 }
+            };
+            // The item names its document's first row, so that the rows are asked for together with the table's entry; where that says another (tables
+            // moved after the list was made), it decides.
+            auto link_rows = [&](int w, const WorkItem& it) {
+                first_row = p.a.a.doc_active_start[it.doc];
+                row_tables(w, it, it.doc_row);
                 id = w < n_units ? page_id(it, lane) : -2;
             };
-            auto link_pages = [&]() {
+            auto link_pages = [&](int w, WorkItem& it) {
+                if (first_row != it.doc_row) {
+                    it.doc_row = first_row;
+                    row_tables(w, it, first_row);
+                }
                 bad = 0;
 #pragma unroll
                 for (int r = 0; r < kRounds; ++r) {
@@ -427,7 +438,7 @@ attn_paged_kernel(const __grid_constant__ Maps maps, const Params p)
                         if (++st == C::NK) { st = 0; k_par ^= 1; }
                         if (++sc == C::NC) { sc = 0; c_par ^= 1; }
                     }
-                    if (t == 0) link_pages();
+                    if (t == 0) link_pages(w1, it1);
                     if (t == 1) link_scales(w1);
                 }
                 if (!ok) break;
