@@ -1106,7 +1106,7 @@ int launch_d(const PagedArgs& a)
     p.G = g.Hq / g.Hkv;
     attn_paged_kernel<D, TWO><<<sm_count(), kThreads, C::SMEM, a.a.stream>>>(maps, p);
     HPD_CUDA_TRY(cudaGetLastError());
-    return launch_attn_merge(a.a);
+    return launch_paged_merge(a.a);
 }
 
 }  // namespace

@@ -924,7 +924,8 @@ hpd_attn_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
 // Merge of the partial results of documents whose prefix was split over several work items.  One warp per (row, q
 // head); the chunks' partials are fetched four at a time so that their loads are in flight together (the kernel is a
 // chain of L2 round trips, not of bytes).
-template <int D>
+// A sum that is NaN: under bf16 caches the row's log-sum-exp is -inf, as in the rows of documents that were not split; over paged caches it is NaN, there too.
+template <int D, bool PAGED>
 __global__ void __launch_bounds__(256)
 hpd_merge_kernel(TcParams p, const DocSplit* split)
 {
@@ -1002,7 +1003,7 @@ hpd_merge_kernel(TcParams p, const DocSplit* split)
         } else {
             *reinterpret_cast<uint32_t*>(op) = pack_bf16(acc[0] * inv, acc[1] * inv);
         }
-        if (p.a.lse && lane == 0) p.a.lse[w] = L == 0.f ? -INFINITY : (M + log2f(L)) * kLn2;
+        if (p.a.lse && lane == 0) p.a.lse[w] = (PAGED ? L != 0.f : L > 0.f) ? (M + log2f(L)) * kLn2 : -INFINITY;
     }
 }
 
@@ -1037,7 +1038,7 @@ TcParams make_params(const AttnArgs& a)
     return p;
 }
 
-template <int D>
+template <int D, bool PAGED>
 int launch_merge(const TcParams& p, bool never_split)
 {
     const AttnArgs& a = p.a;
@@ -1048,7 +1049,7 @@ int launch_merge(const TcParams& p, bool never_split)
     const long long merge_cap = static_cast<long long>(a.n_docs) * a.g.Hkv < 4ll * n_sm ? 8ll * n_sm : 2ll * n_sm;
     const int merge_grid = never_split ? 1 : static_cast<int>(std::min<long long>(std::max<long long>(merge_blocks, 1), merge_cap));
     const DocSplit* split = reinterpret_cast<const DocSplit*>(static_cast<char*>(a.workspace) + a.lay.off_split);
-    HPD_CUDA_TRY(launch_chained(hpd_merge_kernel<D>, merge_grid, 256, 0, a.stream, p, split));
+    HPD_CUDA_TRY(launch_chained(hpd_merge_kernel<D, PAGED>, merge_grid, 256, 0, a.stream, p, split));
     return HPD_OK;
 }
 
@@ -1112,18 +1113,16 @@ int launch_d(const AttnArgs& a)
         }
     }
     HPD_CUDA_TRY(launch_chained(hpd_attn_tc_kernel<D, MODE>, n_sm, kThreadsOf<MODE>, C::SMEM, a.stream, mq, mk, mv, mbk, mbv, sm, p));
-    return launch_merge<D>(p, MODE == kPrefill);
-}
-
-template <int D>
-int launch_split_merge(const AttnArgs& a)
-{
-    return launch_merge<D>(make_params(a), false);
+    return launch_merge<D, false>(p, MODE == kPrefill);
 }
 
 }  // namespace
 
-int launch_attn_merge(const AttnArgs& a) { return a.g.D == 128 ? launch_split_merge<128>(a) : launch_split_merge<64>(a); }
+int launch_paged_merge(const AttnArgs& a)
+{
+    const TcParams p = make_params(a);
+    return a.g.D == 128 ? launch_merge<128, true>(p, false) : launch_merge<64, true>(p, false);
+}
 
 int launch_attn_tc(const AttnArgs& a)
 {

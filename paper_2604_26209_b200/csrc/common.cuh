@@ -176,7 +176,7 @@ int launch_merge_lse(const hpd_geom& g, int max_rows, const int32_t* n_active, c
                      const __nv_bfloat16* o_b, const float* lse_b, __nv_bfloat16* o, float* lse, cudaStream_t stream);
 int launch_append_paged(const hpd_geom& g, const AppendPagedArgs& a);
 int launch_attn_paged(const PagedArgs& p);
-int launch_attn_merge(const AttnArgs& a);    // the partial results of split documents, and the ticket counter rewound
+int launch_paged_merge(const AttnArgs& a);   // behind launch_attn_paged: the partial results of split documents, and the ticket counter rewound
 int launch_attn_std(const StdArgs& a);         // TMA ring + warp-level tensor-core instructions
 int launch_attn_tc(const AttnArgs& a);       // tcgen05 / TMA kernel
 
