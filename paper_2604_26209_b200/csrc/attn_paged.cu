@@ -932,9 +932,10 @@ attn_paged_kernel(const __grid_constant__ Maps maps, const Params p)
                 M_row = fmaxf(M, other.x);
                 l_row = (M == -INFINITY ? l : l * ex2(M - M_row)) + (other.x == -INFINITY ? other.y : other.y * ex2(other.x - M_row));
             }
-            // o = O 2^(R - 7 - M) / l, the power in two steps: it may be that of any V scale; a partial result leaves the division out
+            // o = O 2^(R - 7 - M) / l, the power in two steps: it may be that of any V scale.  So are partial results: without the division, values of one
+            // sign above 2^(119 - log2 of the chunk's tokens) could leave fp32 before the merge divides.
             const float two = R == -INFINITY ? 0.f : ex2(0.5f * (R - kUp - M_row));
-            const float inv = two * (l_row == 0.f ? 0.f : final_out || l_row != l_row ? 1.f / l_row : 1.f);
+            const float inv = two * (l_row == 0.f ? 0.f : 1.f / l_row);
             const int64_t pr = (static_cast<int64_t>(final_out ? 0 : u.part_base) + u.row_begin + b_row) * p.a.a.g.Hq + hq;
             float* po = p.part_o + pr * D;
             // the accumulator, 32 columns at a time; rolled: the code runs once per unit, out of a cold instruction cache

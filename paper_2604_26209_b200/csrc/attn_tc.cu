@@ -924,6 +924,7 @@ hpd_attn_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
 // Merge of the partial results of documents whose prefix was split over several work items.  One warp per (row, q
 // head); the chunks' partials are fetched four at a time so that their loads are in flight together (the kernel is a
 // chain of L2 round trips, not of bytes).
+// A chunk's partial result: over paged caches its weighted mean of the values, which is a number wherever they are; under bf16 caches that mean times its sum.
 // A sum that is NaN: under bf16 caches the row's log-sum-exp is -inf, as in the rows of documents that were not split; over paged caches it is NaN, there too.
 template <int D, bool PAGED>
 __global__ void __launch_bounds__(256)
@@ -956,16 +957,25 @@ hpd_merge_kernel(TcParams p, const DocSplit* split)
         const int rows_d = p.a.doc_active_start[d + 1] - das;
         const int64_t pr0 = (static_cast<int64_t>(sp.part_base) + (r - das)) * Hq + h;      // chunk c: pr0 + c * step
         const int64_t step = static_cast<int64_t>(rows_d) * Hq;
-        float M = -INFINITY;
+        float M = -INFINITY, L = 0.f;
         for (int c0 = 0; c0 < sp.n_chunks; c0 += kBatch) {
-            float m[kBatch];
+            float m[kBatch], l[PAGED ? kBatch : 1];
 #pragma unroll
-            for (int i = 0; i < kBatch; ++i)
+            for (int i = 0; i < kBatch; ++i) {
                 m[i] = c0 + i < sp.n_chunks ? p.part_ml[(pr0 + (c0 + i) * step) * 2] : -INFINITY;
+                if constexpr (PAGED) l[i] = c0 + i < sp.n_chunks ? p.part_ml[(pr0 + (c0 + i) * step) * 2 + 1] : 0.f;
+            }
+            const float was = M;
 #pragma unroll
             for (int i = 0; i < kBatch; ++i) M = fmaxf(M, m[i]);
+            if constexpr (PAGED) {                       // the sum is needed before the first partial result: they are weighted means
+                if (M != was) L *= exp2f(was - M);
+#pragma unroll
+                for (int i = 0; i < kBatch; ++i) L = fmaf(m[i] == -INFINITY ? 0.f : exp2f(m[i] - M), l[i], L);
+            }
         }
-        float L = 0.f, acc[E];
+        const float share = PAGED && L != 0.f ? 1.f / L : 0.f;
+        float acc[E];
 #pragma unroll
         for (int e = 0; e < E; ++e) acc[e] = 0.f;
         for (int c0 = 0; c0 < sp.n_chunks; c0 += kBatch) {
@@ -988,12 +998,13 @@ hpd_merge_kernel(TcParams p, const DocSplit* split)
             for (int i = 0; i < kBatch; ++i) {
                 if (c0 + i >= sp.n_chunks) continue;
                 const float f = ml[i].x == -INFINITY ? 0.f : exp2f(ml[i].x - M);
-                L += f * ml[i].y;
+                if constexpr (!PAGED) L += f * ml[i].y;
+                const float w = PAGED ? f * ml[i].y * share : f;
 #pragma unroll
-                for (int e = 0; e < E; ++e) acc[e] = fmaf(f, o[i][e], acc[e]);
+                for (int e = 0; e < E; ++e) acc[e] = fmaf(w, o[i][e], acc[e]);
             }
         }
-        const float inv = L > 0.f ? 1.f / L : 0.f;
+        const float inv = PAGED ? 1.f : L > 0.f ? 1.f / L : 0.f;
         __nv_bfloat16* op = p.a.o + w * D + lane * E;
         if constexpr (E == 4) {
             uint2 v;
