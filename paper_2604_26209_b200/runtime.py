@@ -187,9 +187,14 @@ class SharedBlockBatch:
 class PagedBatch:
     """One layer's decode state over paged caches in 8 bits: the documents in pages of ``page_size`` tokens, every branch in a page of suffix_cap tokens of
     a second pool.  A step is ``build_meta`` -> ``append`` (rotation and quantisation of the step's tokens) -> ``attn``; the caches are filled from a
-    batch's bf16 tensors by the same append, the documents in one call, the branches' earlier tokens step by step."""
+    batch's bf16 tensors by the same append, the documents in one call, the branches' earlier tokens step by step.
 
-    def __init__(self, s: Structure, t: Dict[str, np.ndarray], page_size: int = 64, device="cuda"):
+    There is no position-order mask over pages: a structure that DeviceBatch would run under it is refused, unless ``posorder=False`` says that its
+    per-slot anchors are anchors only."""
+
+    def __init__(self, s: Structure, t: Dict[str, np.ndarray], page_size: int = 64, device="cuda", posorder: Optional[bool] = None):
+        if (s.slot_vis is not None) if posorder is None else posorder:
+            raise B.HpdError("PagedBatch: the position-order mask reads bf16 caches (DeviceBatch); posorder=False: the structure's anchors are anchors only")
         db = DeviceBatch(s, t, device, posorder=False)
         self.db, self.s, self.g = db, s, s.geom
         i32 = lambda a: torch.from_numpy(np.ascontiguousarray(a, dtype=np.int32)).to(device)
