@@ -301,7 +301,8 @@ int hpd_prefill_attn(const hpd_geom* geom /*host*/, int n_docs, int total_tokens
  * n_pages pages of page_size tokens.  A page holds, for every kv head, e4m3 codes of its keys and of its values and one scale each:
  *   page_k, page_v              [n_pages, Hkv, page_size, D]  e4m3 (one byte: sign, 4 exponent bits, 3 fraction bits; no infinities)
  *   page_k_scale, page_v_scale  [n_pages, Hkv]                e8m0 (one byte b: 2^(b-127); 255: NaN)
- *   value = code * scale.  A cached element is within 2^-4 of itself of what was appended (2^-10 of the scale below 2^-6 of it).
+ *   value = code * scale.  A finite element is within 2^-4 of itself of what was appended (keys: of the rotated key in bf16) or, where that is more, within
+ *   2^-10 of the page's scale; within 2^-9 of it where the scale has grown since (what falls below 2^-6 of a scale is rounded again when it grows).
  * Sequences -- documents, branches -- own pages through a table int32 [table_rows, pages_per_seq]: token t of a sequence is token
  * t % page_size of page table[t / page_size].  No two sequences that are appended to may own the same page; for reading, documents may share pages.
  *
@@ -320,7 +321,8 @@ int hpd_prefill_attn(const hpd_geom* geom /*host*/, int n_docs, int total_tokens
  *   The rotated key is rounded to bf16 as by hpd_rope and quantised from there.  Scales are powers of two: for the tokens that a call puts
  *   into a page, the smallest 2^n >= 2^-126 with (largest finite magnitude) <= 448 * 2^n; a page that held tokens keeps its scale where that is
  *   larger, and where it is smaller the codes held are multiplied by the quotient and rounded.  Codes are rounded to nearest (even);
- *   infinities become the largest code, NaN stays NaN.  Bytes of a page behind its last token are not touched.
+ *   infinities become the largest code of the scale that they meet, a number like any other from then on; NaN stays NaN.  Bytes of a page behind its last
+ *   token are not touched.
  *   A token beyond pages_per_seq * page_size sets HPD_S_OVERFLOW, a table entry out of range HPD_S_BAD_TABLE; nothing is stored for it, its q is rotated.
  */
 int hpd_append_paged(const hpd_geom* geom /*host*/, int n_seqs, int max_rows, const int32_t* n_rows /*dev*/,
