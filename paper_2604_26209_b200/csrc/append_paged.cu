@@ -5,11 +5,13 @@
 //     n = smallest integer >= -126 with a <= 448 * 2^n
 //     e = n for a page that held no token, else max(n, e of before); codes held before become e4m3(code * 2^(e_before - e))
 //     new codes = e4m3(x * 2^-e)
-// Roundings: the key to bf16 (2^-8 of it), the code (2^-4 of the value).  The angle is reduced in 64 bits and rounded to 32 as hpd_rope does it, so that keys
+// Roundings: the key to bf16 (2^-8 of it), the code (2^-4 of the value, 2^-10 of the scale below 2^-6 of it), codes held before that fall below 2^-6 of a
+// grown scale once more (2^-10 of that scale each time, 2^-9 of the last one in all).  The angle is reduced in 64 bits and rounded to 32 as hpd_rope does it, so that keys
 // that hpd_rope has rotated and keys rotated here give the same codes; against a rotation in 64 bits up to some ten in 3.5 million codes lie on the
 // other side of a border, one step off (with sines and cosines rounded once: up to four).
 // With powers of two as scales the growth of a scale is exact for every code that stays a normal number, so a page that fills up
-// token by token ends with the codes of one that is filled at once, but for elements below 2^-14 of the largest.
+// token by token ends with the codes of one that is filled at once, but for infinities and for elements below 2^-6 of the final scale (up to 2^-13.8 of the
+// page's largest element, which is above 224 scales).
 //
 // HBM bound: a token's q, k and v are read once, the codes written once; what a page holds is read only where its scale grows.
 // Ordinary launches: the kernels before have ended when these start.

@@ -1,4 +1,4 @@
-"""How far a cached element may be from what was appended.
+"""How far a cached element may be from what was appended, and when a page that fills up token by token holds the codes of one that is filled at once.
 
 A code is off by half a step: 2^-4 of a normal element, 2^-10 of the scale below 2^-6 of it.  Where a scale s grows to s' >= 2 s, an element that stays a
 normal code does not change; one that falls below 2^-6 s' is rounded again, to a multiple of 2^-9 s': by 2^-10 s' at most.  It was off by less
@@ -41,6 +41,10 @@ def test_pages_filled_token_by_token(seed):
         # from what was appended
         assert np.all(np.abs(many.tokens([0], n)[0] - x) <= np.maximum(np.abs(x) * 2.0 ** -4, scale * 2.0 ** -9))
         assert np.all(np.abs(one.tokens([0], n)[0] - x) <= np.maximum(np.abs(x) * 2.0 ** -4, scale * 2.0 ** -10))
+        # from the page filled at once
+        normal = np.abs(x[:, 0]) >= scale * 2.0 ** -6
+        assert np.array_equal(one.k[0, 0, :n][normal], many.k[0, 0, :n][normal])
+        assert np.all(np.abs(po.VALUES[one.k] - po.VALUES[many.k]) <= 2.0 ** -9)
 
 
 def test_an_element_rounded_twice():
@@ -53,6 +57,20 @@ def test_an_element_rounded_twice():
     p.append(0, 1, np.full((1, 1, 64), 896.0), np.full((1, 1, 64), 896.0))
     off = abs(p.tokens([0], 1)[0][0, 0, 0] - x)
     assert po.scale_value(p.ks)[0, 0] == 2 and 2 * 2.0 ** -10 < off <= 2 * 2.0 ** -9
+
+
+def test_the_same_codes_reach_down_to_2_to_the_minus_6_of_the_scale_only():
+    """The largest element of a page may be just above 224 scales: an element of more than 2^-14 of it can be rounded twice."""
+    x = float(_bf16(np.array([0.01428]))[0])
+    top = 225.0
+    assert x > 2.0 ** -14 * top and x < 2.0 ** -6
+    one, many = _empty(), _empty()
+    tokens = np.zeros((4, 1, 64))
+    tokens[:, 0, 0] = x, 0.25 * top, 0.5 * top, top
+    one.append(0, 0, tokens, tokens)
+    for t in range(4):
+        many.append(0, t, tokens[t:t + 1], tokens[t:t + 1])
+    assert one.ks[0, 0] == many.ks[0, 0] == 127 and one.k[0, 0, 0, 0] != many.k[0, 0, 0, 0]
 
 
 def test_infinities_keep_the_largest_code_of_the_scale_that_they_met():
