@@ -930,7 +930,8 @@ template <int D, bool PAGED>
 __global__ void __launch_bounds__(256)
 hpd_merge_kernel(TcParams p, const DocSplit* split)
 {
-    // The attention kernel lets this one in only after its own wait, so the plan, written by a kernel before it, can be read now.  As a rule
+    // When this one comes, the kernel before the attention, which wrote the plan, has ended: hpd_attn_tc_kernel lets it in only after its own wait,
+    // attn_paged_kernel is an ordinary launch.  So the plan can be read now.  As a rule
     // nothing was split: then all blocks but one end at once, most of them while the attention still runs, and that one holds the
     // order of the stream (a kernel that waits for this grid thereby waits for the attention).  With every block waiting and then reading
     // the plan, a step of 8 prompts spent its last 2.3 us here (attention call 27.4 -> 25.2 us, of 16 prompts 47.7 -> 45.7).
