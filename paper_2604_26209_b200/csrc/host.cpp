@@ -2,8 +2,9 @@
 //
 // A decode step of few prompts keeps the GPU busy for 20 to 40 us; marshalling its three calls (some fifty tensors) through
 // ctypes objects took longer than that.  Every entry point here takes (geometry, arguments of the C function in order
-// without the stream): tensors become device pointers (device-resident contiguous ones only), None a null pointer; the current
-// stream is appended.  The functions' addresses come from the library that binding.load() has opened.
+// without the stream): tensors become device pointers (contiguous ones of the current device only: a kernel on
+// another device's stream would fault at their addresses), None a null pointer; the current stream is appended.  The functions' addresses
+// come from the library that binding.load() has opened.
 #include <Python.h>
 
 #include <cstring>
@@ -38,7 +39,14 @@ bool read_geom(PyObject* o, hpd_geom& g)
     return true;
 }
 
-template <typename T> bool convert(PyObject* o, T& out)
+bool other_device()
+{
+    PyErr_SetString(PyExc_AssertionError, "tensors of the current device only");
+    return false;
+}
+
+// device: the tensors' so far, -1 before the first
+template <typename T> bool convert(PyObject* o, T& out, int& device)
 {
     if constexpr (std::is_pointer_v<T>) {
         if (o == Py_None) { out = nullptr; return true; }
@@ -51,6 +59,8 @@ template <typename T> bool convert(PyObject* o, T& out)
             PyErr_SetString(PyExc_AssertionError, "device-resident contiguous tensors only");
             return false;
         }
+        if (device < 0) device = t.get_device();
+        else if (t.get_device() != device) return other_device();
         out = static_cast<T>(t.data_ptr());
         return true;
     } else {
@@ -67,8 +77,14 @@ PyObject* invoke_with(int (*f)(const hpd_geom*, A...), PyObject* const* args, st
 {
     std::tuple<A...> v;
     hpd_geom g;
-    if (!read_geom(args[0], g) || !(convert(args[1 + I], std::get<I>(v)) && ...)) return nullptr;
-    std::get<sizeof...(A) - 1>(v) = c10::cuda::getCurrentCUDAStream().stream();
+    int device = -1;
+    if (!read_geom(args[0], g) || !(convert(args[1 + I], std::get<I>(v), device) && ...)) return nullptr;
+    const c10::cuda::CUDAStream stream = c10::cuda::getCurrentCUDAStream();
+    if (device >= 0 && device != stream.device_index()) {
+        other_device();
+        return nullptr;
+    }
+    std::get<sizeof...(A) - 1>(v) = stream.stream();
     int rc;
     Py_BEGIN_ALLOW_THREADS
     rc = std::apply([&](auto... a) { return f(&g, a...); }, v);
