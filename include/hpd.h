@@ -337,12 +337,15 @@ int hpd_append_paged(const hpd_geom* geom /*host*/, int n_seqs, int max_rows, co
  *     o = softmax(sm_scale * q . [K_d ; K_s]^T) [V_d ; V_s]
  * over the document's doc_prefix_len[d] tokens in the pages that doc_page[d] names (page_size 16, 32 or 64) and the branch's tokens in
  * page slot_page[s] of the branches' pool, whose pages hold suffix_cap tokens.  A document's pages are read from memory once per kv head for all
- * of its rows.  Scores, softmax and sums are held in fp32; probabilities are rounded to fp16, codes enter the products exactly.
+ * of its rows.  Scores, softmax and sums are held in fp32; probabilities are rounded to fp16, codes enter the products exactly.  A row of q (of one head)
+ * enters as two e4m3 terms of its elements, relative to its largest: elements of at least 2^-8 of that exactly, smaller ones to 2^-17 of it.  Products of a
+ * probability and a page's V scale that are below 2^-60 of the row's largest take part in the sum alone.
  *   q [max_rows, Hq, D] bf16 (rotated); doc_page [n_docs, pages_per_doc], slot_page [n_slots] int32 (dev); tables and workspace from
  *   hpd_build_meta (active_slot, suffix_len, ...); suffix_includes_new, o, lse as hpd_attn_decode.  Documents may share pages.
  *   The workspace holds the step's plan and the call's partial results: calls that share one follow each other in a stream, as with hpd_attn_decode.
  *   What lies in a page behind its last token, NaN included, has no influence.  A NaN code in a document's key or value reaches the rows of that document
- *   alone, one of a branch that branch's rows alone (all of their elements); a row whose q holds an infinity or NaN is NaN.
+ *   alone, one of a branch that branch's rows alone (all of their elements); a row whose q holds an infinity or NaN is NaN (zeros
+ *   and -inf, as any other, where it sees no token).
  *   A document's page out of range sets HPD_S_BAD_TABLE and makes that document's rows NaN; so does a document longer than
  *   pages_per_doc * page_size.  A branch's page out of range sets HPD_S_BAD_TABLE and its rows see the document only.
  */

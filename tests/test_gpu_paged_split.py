@@ -114,3 +114,16 @@ def test_values_at_the_top_of_the_range(name, v_exp):
     c = _case(name, change)
     assert bool(torch.isfinite(c.o.float()).all())
     c.check(some=30)
+
+
+@pytest.mark.parametrize("heads", [(4, 1, 64), (8, 2, 128)])
+def test_rows_that_see_nothing_whatever_their_queries(heads):
+    """Zeros and -inf for a row without a token, an infinity or NaN in its q or not; a row with tokens is NaN."""
+    c = Case(heads, 32, [0, 5], [3, 2], 4, depth=[0, 0, 1, 0, 0], seed=2)
+    c.q[0, 0, 3], c.q[1, 0, 3], c.q[2, 0, 3], c.q[3, 0, 3] = float("inf"), float("nan"), float("nan"), float("inf")
+    c.upload()
+    c.attend(new=False)
+    torch.cuda.synchronize()
+    assert bool((c.o[:2] == 0).all()) and bool(torch.isneginf(c.lse[:2]).all())
+    assert bool(torch.isnan(c.o[2:4, 0]).all()) and bool(torch.isnan(c.lse[2:4, 0]).all())
+    assert bool(torch.isfinite(c.o[2:, 1:].float()).all()) and int(c.m.dev_status.item()) == 0
