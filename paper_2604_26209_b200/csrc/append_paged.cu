@@ -232,8 +232,8 @@ append_step_kernel(int Hq /* 0: no queries */, int Hkv, const InvFreq inv_freq, 
 // segments that begin in its window of rows and takes them in groups of up to 64 rows, for every gridDim.y-th kv head and those heads' queries:
 // the angles of a group's rows are computed once, each thread those of one frequency (its frequency and the rows' position IDs fetched with the
 // tables: 586 -> 575 us and 22.6 -> 18.5; from the table of parameters lane by lane and from memory row by row they were a third of a small call).
-// 64 prompts of 2288 tokens (32 / 8 heads of 128, pages of 64): 575 us, 5.7 TB/s.  What few rows cost is a group's chain -- tables, pages, scales,
-// then two round trips per head: 7.5 us for one prompt, 18.5 for 37 ragged chunks.
+// 64 prompts of 2288 tokens (32 / 8 heads of 128, pages of 64): 577 to 591 us from box to box, 5.5 to 5.7 TB/s.  What few rows cost is a group's chain --
+// tables, pages, scales, then two round trips per head: 7.5 to 8.2 us for one prompt without rotation, 18.5 to 20.5 for 37 ragged chunks.
 // ------------------------------------------------------------------------------------------------
 constexpr int kTokThreads = 256, kTokRows = 64, kTokQueries = 2;
 template <int D> constexpr int kTokResident = D == 128 ? 3 : 4;       // CTAs of an SM
@@ -417,7 +417,8 @@ int launch_append_paged(const hpd_geom& g, const AppendPagedArgs& a)
         // A window's segments should be one group of up to 64 rows: windows of 48, but 64 for large pages while every window and head has a CTA at the
         // same time.  In us with windows of 64 / 48 / 32 rows: 37 ragged chunks in pages of 16 24.6 / 18.5 / 21.8, of 32 23.3 / 23.0 / 20.7, of 64
         // 24.7 / 25.5 / 32.6; 64 prompts of 2288 tokens in pages of 16 572 / 560 / 596, of 32 576 / 572 / 593, of 64 590 / 575 / 571; one
-        // prompt in pages of 64 7.6 / 8.1 / 10.1.
+        // prompt in pages of 64 7.6 / 8.1 / 10.1.  (The chunks with 8 / 4 heads of 64, the rest with 32 / 8 of 128.  With heads of 64 the rule is not the best
+        // everywhere: 8 prompts in pages of 16 22.7 / 28.6 / 26.9, 64 prompts 132 / 142 / 144 in pages of 16, 129 / 141 / 142 of 32, 129 / 132 / 120 of 64.)
         const unsigned resident = static_cast<unsigned>(wide ? kTokResident<128> : kTokResident<64>) * sm_count();
         const unsigned rows = static_cast<unsigned>(a.max_rows), all = static_cast<unsigned>(kTokRows), heads = static_cast<unsigned>(g.Hkv);
         const unsigned window = a.page_size > 32 && (rows + all - 1) / all * heads <= resident ? all : 48;
@@ -425,7 +426,10 @@ int launch_append_paged(const hpd_geom& g, const AppendPagedArgs& a)
         // The heads of a window go to several CTAs, each with tables and angles of its own: as many as fit the GPU at once, and no more than three heads to
         // a CTA until the windows alone are several rounds of it.  Prompts of 2288 tokens, 1 / 2 / 4 / 8 / 16 / 32 / 64 of them, in us: one CTA
         // 57 / 62 / 94 / 113 / 194 / 317 / 574, two 35 / 42 / 64 / 102 / 167 / 311 / 575, three 29 / 35 / 55 / 88 / 161 / 307 / 586,
-        // four 25 / 33 / 62 / 94 / 170 / 320 / 609, eight 20.6 / 35 / 59 / 102 / 190 / 367 / 710.
+        // four 25 / 33 / 62 / 94 / 170 / 320 / 609, eight 20.6 / 35 / 59 / 102 / 190 / 367 / 710.  That is with 8 heads of 128.  4 of 128, 8 / 16 / 64 / 72
+        // prompts: one CTA 82 / 161 / 492 / 529, two (the rule's up to 54 prompts) 89 / 140 / 493 / 548, three 76 / 140 / 511 / 571.  Below the
+        // threshold and above, 54 and 72 prompts: 8 of 128 one 487 / 612, three (the rule's at 54) 497 / 656; 4 of 128 one 421 / 529, two 417 / 548.  With heads
+        // of 64 one CTA would be faster from 16 prompts on: 8 heads, 16 / 64 prompts, one 60 / 204, three (the rule's) 67 / 234; 4 heads 36 / 113 against 40 / 129.
         const unsigned fit = std::max(1u, resident / windows), few = windows < 6 * resident ? (heads + 2) / 3 : 1;
         const dim3 grid(windows, std::min(heads, std::max(fit, few)));
         if (wide) append_tokens_kernel<128><<<grid, kTokThreads, 0, a.stream>>>(Hq, g.Hkv, static_cast<int>(window), f, p);

@@ -21,9 +21,9 @@
 // NaN.  The pages of a document are all its rows' in any case.  Branches share tiles, and 0 * NaN would reach the others: a NaN among a branch's V
 // codes is zeroed and noted, and its rows become NaN in the epilogue; one among its K codes stays in its own columns, which others' rows mask.
 //
-// What bounds it.  64 prompts (256 documents of 512 tokens with 24 branches each, 32 / 8 heads of 128): 165 us for 72.7 us of bytes at the copy rate
+// What bounds it.  64 prompts (256 documents of 512 tokens with 24 branches each, 32 / 8 heads of 128): 166 us for 72.7 us of bytes at the copy rate
 // and 146 us of hpd_attn_decode over an unpaged bf16 cache of twice the bytes; 192 documents of 1024 to 4096 tokens with 12 branches: 290 for 165,
-// and 369 in bf16 (after a second of it, at the clock that the power cap leaves, 178 and 342).  The copies and matrix products alone take 105 of the 165 us
+// and 369 in bf16 (after a second of it, at the clock that the power cap leaves, 172 to 178 and 330 to 344).  The copies and matrix products alone take 105 of the 166 us
 // (a product of 128 x 64 x 16 or 32 takes the tensor core 48 to 64 cycles here whatever its type: 12 of them per tile); the softmax of a tile
 // is a chain of 1.9 k cycles for its warp, 2.3 k with both pipelines' on the SM's issue slots (41 % used), which is why units of few rows
 // are taken apart (ways_of); a unit's turn costs 8 k cycles (Q fetched and split 5 k, epilogue 3 k), of which the other pipeline covers about half.
@@ -1114,7 +1114,8 @@ int launch_d(const PagedArgs& a)
 
 int launch_attn_paged(const PagedArgs& a)
 {
-    // few rows to a document on average, or few documents (whose units are halved then)
+    // Few rows to a document on average, or few documents (whose units are halved then).  By the rows that there may be: how many of them are live only
+    // the device knows, so a step whose branches have mostly retired keeps the kernel of the full one.
     const long long rows = static_cast<long long>(a.a.max_rows) * (a.a.g.Hq / a.a.g.Hkv);
     const bool two = rows <= static_cast<long long>(a.a.n_docs) * (kM / 2) || 2ll * a.a.n_docs * a.a.g.Hkv <= sm_count();
     if (a.a.g.D == 128) return two ? launch_d<128, true>(a) : launch_d<128, false>(a);
